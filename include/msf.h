@@ -50,7 +50,9 @@ typedef enum msf_status {
     MSF_ERR_CUDA = 3,         /* a CUDA runtime call failed; see msf_last_cuda_error */
     MSF_ERR_TIMEOUT = 4,      /* a device-side wait hit its bound (kernel returned early) */
     MSF_ERR_STATE = 5,        /* plan not bound, or history operation not allowed */
-    MSF_ERR_WORKSPACE = 6     /* workspace smaller than msf_plan_query reports */
+    MSF_ERR_WORKSPACE = 6,    /* workspace smaller than msf_plan_query reports */
+    MSF_ERR_PAGES = 7,        /* a cache's pool or a sequence's table is full (msf_cache.h) */
+    MSF_ERR_NONFINITE = 8     /* values appended to a cache were not finite (msf_cache.h) */
 } msf_status;
 
 typedef enum msf_dtype { MSF_DTYPE_BF16 = 0, MSF_DTYPE_F32 = 1 } msf_dtype;

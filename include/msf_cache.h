@@ -1,0 +1,178 @@
+/*
+ * msf_cache.h - a paged key/value cache in 4 bits: quantising append, attention
+ * over it, and its pages.
+ *
+ * The history ring of msf.h holds a fixed number of bf16 frames of each stream.
+ * This cache holds any number of tokens of many sequences (a stream, one scale
+ * of a stream, a beam) at 9/16 of a byte a value: 3.6 times less than bf16. Its
+ * attention can be joined with an attention over other keys (the window and the
+ * sink, msf_mssa_forward_lse) by that attention's row log-sum-exp, which gives
+ * the attention over both (Eq. 4's softmax over sink, history and window).
+ *
+ * Format. 16 neighbours along the head share a scale. A value is
+ *   code * scale * 2^exponent
+ * with code one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (a sign, two
+ * exponent bits and a mantissa bit: e2m1), scale an 8-bit floating point number
+ * (e4m3) of at least 2^-9, and exponent one number for all keys and one for all
+ * values of the cache. Of a block with largest magnitude a:
+ *   scale = e4m3(a / (6 * 2^exponent)), at least 2^-9 and at most 448,
+ *   code  = e2m1(x / (scale * 2^exponent)), at most 6,
+ * both to the nearest, ties to even. Values held are exact in bf16. A value that
+ * is not finite is held as 0 (NaN) or as the block's largest code (an infinity:
+ * a counts it as the largest finite bf16), and the append that meets one raises
+ * NONFINITE in the device status, so that nothing read out of the cache is ever
+ * infinite or NaN.
+ *
+ * Pages. A page holds page_tokens tokens of every head and layer; the pool is
+ * [layers][pages][page_bytes]. Each sequence has a length and a table of the
+ * pages that hold its tokens, each page a count of the tables that name it, all
+ * on the device (the state): no call waits for the host, and every call can be
+ * captured in a graph. New pages are always the free ones of the lowest number,
+ * given to the sequences in the order of the call's list.
+ *
+ * Conventions are those of msf.h: caller-owned buffers, 16-byte aligned, calls
+ * asynchronous on `stream` and ordered by the caller. Lists (seqs, counts, ...)
+ * are int32 device arrays, read when the call runs on the device. What only the
+ * device can check (a sequence number outside the cache, one that a list names
+ * twice, a negative count, no page left, a sequence longer than its table) is
+ * raised in the device status: the call changes nothing then, and neither does
+ * any call that would change the cache until msf_cache_device_status has read
+ * the status.
+ */
+#ifndef MSF_CACHE_H
+#define MSF_CACHE_H
+
+#include "msf.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct msf_cache_desc {
+    int32_t layers;          /* >= 1 */
+    int32_t kv_heads;        /* Hk >= 1 */
+    int32_t head_dim;        /* D: 64 or 128 */
+    int32_t page_tokens;     /* P: 16, 32, 64 or 128 */
+    int32_t pages;           /* of the pool, 1 .. 2^24 */
+    int32_t sequences;       /* S, 1 .. 65536 */
+    int32_t sequence_pages;  /* table entries of a sequence: it holds up to sequence_pages * P tokens (below 2^31) */
+    int32_t k_exponent;      /* of all keys, -64 .. 64 */
+    int32_t v_exponent;      /* of all values, -64 .. 64 */
+} msf_cache_desc;
+
+typedef struct msf_cache_info {
+    uint64_t pool_bytes;       /* layers * pages * page_bytes */
+    uint64_t page_bytes;       /* one layer of a page: Hk * P * D * 9 / 8 */
+    uint64_t state_bytes;      /* status, lengths, tables, counts: what a checkpoint saves beside the pool */
+    uint64_t workspace_bytes;  /* lists of a call, partial results of the attention */
+    uint64_t lengths_offset;   /* in the state: int32 [S] tokens of each sequence */
+    uint64_t table_offset;     /* int32 [S][sequence_pages] page numbers, -1 past a sequence's last page */
+    uint64_t refs_offset;      /* int32 [pages] tables that name a page; 0: free */
+} msf_cache_info;
+
+typedef struct msf_cache* msf_cache_t;
+
+/* Host only. Errors: INVALID_ARG (null pointers, sizes out of range),
+ * UNSUPPORTED (head_dim, page_tokens). */
+msf_status msf_cache_create(const msf_cache_desc* desc, msf_cache_t* out);
+void msf_cache_destroy(msf_cache_t cache);
+msf_status msf_cache_query(msf_cache_t cache, msf_cache_info* info);
+
+/* Attach the buffers. Empties the cache: all lengths 0, all pages free (the
+ * pool's bytes stay as they are). A saved state copied over `state` afterwards
+ * takes up where it was. Completed before returning. Errors: INVALID_ARG,
+ * WORKSPACE (a buffer smaller than msf_cache_query reports), CUDA. */
+msf_status msf_cache_bind(msf_cache_t cache, void* pool, size_t pool_bytes, void* state, size_t state_bytes,
+                          void* workspace, size_t workspace_bytes);
+
+/* Room for counts[i] (or, with counts NULL, `tokens`) more tokens of sequence
+ * seqs[i] (NULL: i), i < n: lengths grow by the counts, pages are taken as
+ * needed, and a last page that is not full and that other tables name too is
+ * copied first (all layers), so that what msf_cache_write puts there stays the
+ * sequence's own. The new tokens' contents are undefined until written. Raises
+ * PAGES on the device when the pool or a table cannot hold the tokens (nothing
+ * grows then). Errors: INVALID_ARG, STATE, CUDA. */
+msf_status msf_cache_grow(msf_cache_t cache, const int32_t* seqs, const int32_t* counts, int32_t tokens, int32_t n,
+                          void* stream);
+
+/* Quantise and write the newest tokens of layer `layer`: k, v bf16
+ * [n][tokens][Hk][D] with element strides {sequence, token, head} (multiples of
+ * 8, the head dimension contiguous), row t < counts[i] (NULL: tokens) at
+ * position length - counts[i] + t of sequence seqs[i] (NULL: i). A row whose
+ * position is negative, or whose page other tables name too, is not written.
+ * Errors: INVALID_ARG, STATE, CUDA. */
+msf_status msf_cache_write(msf_cache_t cache, int32_t layer, const int32_t* seqs, const int32_t* counts, int32_t n,
+                           int32_t tokens, const void* k, const void* v, const int64_t strides[3], void* stream);
+
+/* Read tokens back as bf16 values: row t of k, v (laid out as for
+ * msf_cache_write) is position begins[i] (NULL: 0) + t, zeros outside the
+ * sequence. Errors: INVALID_ARG, STATE, CUDA. */
+msf_status msf_cache_read(msf_cache_t cache, int32_t layer, const int32_t* seqs, const int32_t* begins, int32_t n,
+                          int32_t tokens, void* k, void* v, const int64_t strides[3], void* stream);
+
+/* msf_cache_fork: the copies get pages of their own. */
+#define MSF_CACHE_FORK_SHARE 0
+#define MSF_CACHE_FORK_COPY 1
+
+/* Sequence dst[i] becomes the first min(length, lengths[i]) tokens (NULL: all)
+ * of sequence src[i], as it was before the call (so a list may permute
+ * sequences, or name a source many times); what dst[i] held is released.
+ * SHARE: the tables name the same pages, and a shared page is copied only when
+ * a sequence grows within it. COPY: the pages are copied (all layers) into pages
+ * that were free before the call. dst names each sequence at most once. Raises
+ * PAGES on the device when a copy finds no pages. Errors: INVALID_ARG, STATE,
+ * CUDA. */
+msf_status msf_cache_fork(msf_cache_t cache, const int32_t* src, const int32_t* dst, const int32_t* lengths, int32_t n,
+                          int32_t flags, void* stream);
+
+/* Sequence seqs[i] (NULL: i) keeps its first lengths[i] tokens (NULL: none);
+ * pages that no table names any more are free. Errors: INVALID_ARG, STATE, CUDA. */
+msf_status msf_cache_truncate(msf_cache_t cache, const int32_t* seqs, const int32_t* lengths, int32_t n, void* stream);
+
+/* Move pages so that the pages in use are the lowest numbers: with u pages in
+ * use, the i-th used page above u moves (all layers) to the i-th free one below,
+ * and tables follow. Errors: STATE, CUDA. */
+msf_status msf_cache_compact(msf_cache_t cache, void* stream);
+
+/* Arguments of msf_cache_attend. Strides in elements. */
+typedef struct msf_cache_attention {
+    const void* q;            /* bf16 [n][queries][heads][D], strides below, the head dimension contiguous */
+    void* out;                /* bf16, as q, with its own strides */
+    float* lse;               /* fp32 [n][heads][queries] (queries contiguous), NULL: not wanted */
+    const void* base_out;     /* another attention's output of the same rows (out's strides), NULL: none */
+    const float* base_lse;    /* and its natural-log log-sum-exp (lse_strides) */
+    int64_t q_strides[3];     /* sequence, query, head: multiples of 8 */
+    int64_t out_strides[3];   /* of out and base_out: multiples of 8 */
+    int64_t lse_strides[2];   /* sequence, head; of lse and base_lse */
+    int32_t queries;          /* a sequence */
+    int32_t heads;            /* a multiple of kv_heads: heads/kv_heads neighbours share keys and values */
+    int32_t causal;           /* 0: every query sees the whole sequence; 1: query i sees its first
+                                 length - queries + 1 + i tokens (the queries are its newest tokens) */
+    float softmax_scale;      /* 0: 1/sqrt(D) */
+} msf_cache_attention;
+
+/* Attention of each sequence's queries over its tokens in layer `layer`,
+ *   out = sum_j softmax_j(softmax_scale q . k_j) v_j,
+ * fp32 scores, softmax and sums; lse = ln sum_j exp(softmax_scale q . k_j). A row
+ * that sees no token has out 0 and lse -infinity. With a base, the result is
+ * the attention over both sets of keys: with L = ln(e^lse + e^base_lse), out =
+ * e^(lse - L) out + e^(base_lse - L) base_out, and lse = L. base_out may be out
+ * and base_lse lse (joined in place); otherwise out and lse may not overlap the
+ * inputs. seqs NULL: sequence i. seqs may name a sequence more than once. Errors:
+ * INVALID_ARG, STATE, UNSUPPORTED (n * heads * queries or strides beyond 2^31
+ * rows), CUDA. */
+msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                            const msf_cache_attention* args, void* stream);
+
+/* Synchronise `stream`, read and clear the device status. In order of weight:
+ * TIMEOUT (a bounded wait gave up), PAGES (no page or table entry left),
+ * INVALID_ARG (a list named a sequence that is none, one twice, or a negative
+ * count), NONFINITE (an append met infinities or NaN, held as said above: the
+ * calls went through), OK. */
+msf_status msf_cache_device_status(msf_cache_t cache, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* MSF_CACHE_H */

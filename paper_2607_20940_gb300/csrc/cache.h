@@ -1,0 +1,109 @@
+// The 4-bit key/value cache shared by its host code and kernels: layouts of the
+// pool, the state and the workspace.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/msf_cache.h"
+
+namespace msf {
+
+constexpr int kCacheBlock = 16;  // values that share a scale, and tokens of a record
+
+// A page of one layer is [Hk][P / 16] records of 16 tokens of a head, each
+//   key codes    [16 tokens][D / 2 bytes]   (two codes a byte, the lower dim in the lower half)
+//   key scales   [16 tokens][D / 16]
+//   value codes  [16 tokens][D / 2 bytes]
+//   value scales [D / 16][16 tokens]
+// so a warp's step over 16 tokens reads 18 D contiguous bytes (18 or 9 lines of
+// 128), keys' scales lie with their token (scores need a token's scales) and
+// values' with their block (outputs need a block's scales of several tokens).
+__host__ __device__ constexpr int cache_record_bytes(int D) { return 18 * D; }
+__host__ __device__ constexpr int cache_k_scales(int D) { return 8 * D; }
+__host__ __device__ constexpr int cache_v_codes(int D) { return 9 * D; }
+__host__ __device__ constexpr int cache_v_scales(int D) { return 17 * D; }
+
+// Words of the state's header.
+enum : int { kCacheStatus = 0, kCacheCopies = 1, kCacheBad = 2, kCacheLive = 3 };
+// Bits of the status word beside kDevTimeout.
+constexpr unsigned kDevPages = 2u, kDevIndex = 4u, kDevNonfinite = 8u;
+constexpr unsigned kCacheStop = kDevPages | kDevIndex;  // nothing changes the cache until these are read
+
+struct CacheView {
+    uint8_t* pool;
+    int L, Hk, D, P, pages, S, W;
+    int log2_p;
+    long long page_bytes;
+    float k_unit, v_unit;  // 2^exponent
+    // state
+    unsigned* head;  // kCacheStatus...
+    int* lengths;    // [S]
+    int* table;      // [S][W]
+    int* refs;       // [pages]
+    unsigned* used;  // [ceil(pages / 32)] bit p % 32 of word p / 32: refs[p] > 0
+    // workspace: lists of one call
+    int* claim;      // [S]
+    int* row;        // [S] first new page of a list's row (grow: times 2, plus 1 if its first is a copied last page)
+    int* new_len;    // [S]
+    int* free_list;  // [pages]
+    int2* copies;    // [pages] (from, to)
+    int* moved;      // [pages] where a page went
+    int* stage;      // [S][W] new table rows
+    // workspace: attention
+    unsigned* counters;  // [kCacheMaxCtas] pieces done of the item that is cut first in a CTA's share
+    float* partials;     // two slots per CTA
+};
+
+constexpr int kCacheMaxCtas = 320;
+// Floats of the attention's partial results.
+constexpr size_t kCachePartialFloats = (size_t)2 * 160 * 256 * 130;
+
+// Page numbers that a table or list holds are checked before use: a state that
+// was copied in from elsewhere may hold anything.
+__host__ __device__ inline bool cache_page_ok(const CacheView& c, int page) {
+    return (unsigned)page < (unsigned)c.pages;
+}
+__host__ __device__ inline int cache_need(const CacheView& c, int tokens) {
+    return (int)(((long long)tokens + c.P - 1) >> c.log2_p);
+}
+
+struct CacheAttnArgs {
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    const uint16_t* base_out;
+    const float* base_lse;
+    long long q_st[3], o_st[3], l_st[2];
+    int queries, heads, group;  // group: heads / Hk
+    int causal;
+    int layer, n;
+    const int* seqs;
+    float scale;
+};
+
+// Launches (host side of the .cu files).
+cudaError_t launch_cache_grow(const CacheView& c, const int* seqs, const int* counts, int tokens, int n, cudaStream_t st);
+cudaError_t launch_cache_fork(const CacheView& c, const int* src, const int* dst, const int* lengths, int n, bool copy,
+                              cudaStream_t st);
+cudaError_t launch_cache_truncate(const CacheView& c, const int* seqs, const int* lengths, int n, cudaStream_t st);
+cudaError_t launch_cache_compact(const CacheView& c, cudaStream_t st);
+struct CacheRows {
+    const int* seqs;
+    const int* at;  // write: counts; read: begins
+    int n, tokens, layer;
+    long long st[3];
+};
+cudaError_t launch_cache_write(const CacheView& c, const CacheRows& r, const uint16_t* k, const uint16_t* v, cudaStream_t st);
+cudaError_t launch_cache_read(const CacheView& c, const CacheRows& r, uint16_t* k, uint16_t* v, cudaStream_t st);
+cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st);
+
+}  // namespace msf
+
+struct msf_cache {
+    msf_cache_desc d;
+    msf_cache_info info;
+    bool bound;
+    msf::CacheView v;
+};

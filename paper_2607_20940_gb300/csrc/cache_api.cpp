@@ -1,0 +1,271 @@
+// C ABI of the 4-bit key/value cache (msf_cache.h): argument checks, buffer
+// layouts, status.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "cache.h"
+#include "internal.h"
+
+namespace {
+
+using msf::CacheView;
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+msf_status cuda_status(cudaError_t e) {
+    if (e == cudaSuccess) return MSF_OK;
+    msf::set_cuda_error((int)e);
+    return MSF_ERR_CUDA;
+}
+
+constexpr size_t kHeadBytes = 256;
+
+// A list of n rows: its length, and arrays that may be NULL.
+bool list_ok(const msf_cache* c, int32_t n, const int32_t* a, const int32_t* b) {
+    return n >= 0 && n <= c->d.sequences && aligned4(a) && aligned4(b);
+}
+
+// Strides of rows of heads: 16-byte vectors, and offsets within 2^62 elements.
+bool strides_ok(const int64_t* s) {
+    for (int i = 0; i < 3; ++i)
+        if (s[i] % 8 || s[i] < 0 || s[i] > (int64_t)1 << 40) return false;
+    return true;
+}
+
+msf_status rows_check(msf_cache_t cache, int32_t layer, const int32_t* seqs, const int32_t* at, int32_t n, int32_t tokens,
+                      const void* k, const void* v, const int64_t* strides) {
+    if (!cache || !strides || layer < 0 || layer >= cache->d.layers || tokens < 0) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    if (!list_ok(cache, n, seqs, at) || !strides_ok(strides)) return MSF_ERR_INVALID_ARG;
+    if (n > 0 && tokens > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return MSF_ERR_INVALID_ARG;
+    return MSF_OK;
+}
+
+msf::CacheRows rows_of(int32_t layer, const int32_t* seqs, const int32_t* at, int32_t n, int32_t tokens,
+                       const int64_t* strides) {
+    msf::CacheRows r;
+    r.seqs = seqs;
+    r.at = at;
+    r.n = n;
+    r.tokens = tokens;
+    r.layer = layer;
+    for (int i = 0; i < 3; ++i) r.st[i] = strides[i];
+    return r;
+}
+
+}  // namespace
+
+extern "C" msf_status msf_cache_create(const msf_cache_desc* desc, msf_cache_t* out) {
+    if (!desc || !out) return MSF_ERR_INVALID_ARG;
+    *out = nullptr;
+    const msf_cache_desc& d = *desc;
+    if (d.layers < 1 || d.layers > 65536 || d.kv_heads < 1 || d.kv_heads > 65536) return MSF_ERR_INVALID_ARG;
+    if (d.pages < 1 || d.pages > 1 << 24 || d.sequences < 1 || d.sequences > 65536 || d.sequence_pages < 1)
+        return MSF_ERR_INVALID_ARG;
+    if (d.k_exponent < -64 || d.k_exponent > 64 || d.v_exponent < -64 || d.v_exponent > 64) return MSF_ERR_INVALID_ARG;
+    if (d.head_dim != 64 && d.head_dim != 128) return MSF_ERR_UNSUPPORTED;
+    if (d.page_tokens != 16 && d.page_tokens != 32 && d.page_tokens != 64 && d.page_tokens != 128)
+        return MSF_ERR_UNSUPPORTED;
+    if ((long long)d.sequence_pages * d.page_tokens >= 1ll << 31) return MSF_ERR_INVALID_ARG;
+
+    msf_cache* c = new (std::nothrow) msf_cache();
+    if (!c) return MSF_ERR_INVALID_ARG;
+    memset((void*)c, 0, sizeof(*c));
+    c->d = d;
+    CacheView& v = c->v;
+    v.L = d.layers;
+    v.Hk = d.kv_heads;
+    v.D = d.head_dim;
+    v.P = d.page_tokens;
+    v.pages = d.pages;
+    v.S = d.sequences;
+    v.W = d.sequence_pages;
+    for (v.log2_p = 4; 1 << v.log2_p < v.P; ++v.log2_p) {
+    }
+    v.page_bytes = (long long)v.Hk * (v.P / msf::kCacheBlock) * msf::cache_record_bytes(v.D);
+    v.k_unit = ldexpf(1.f, d.k_exponent);
+    v.v_unit = ldexpf(1.f, d.v_exponent);
+
+    using msf::round256;
+    msf_cache_info& i = c->info;
+    i.page_bytes = (uint64_t)v.page_bytes;
+    i.pool_bytes = (uint64_t)v.L * v.pages * i.page_bytes;
+    i.lengths_offset = kHeadBytes;
+    i.table_offset = i.lengths_offset + round256((size_t)v.S * 4);
+    i.refs_offset = i.table_offset + round256((size_t)v.S * v.W * 4);
+    i.state_bytes = i.refs_offset + round256((size_t)v.pages * 4) + round256((size_t)(v.pages + 31) / 32 * 4);
+    i.workspace_bytes = 3 * round256((size_t)v.S * 4) + 2 * round256((size_t)v.pages * 4) + round256((size_t)v.pages * 8) +
+                        round256((size_t)v.S * v.W * 4) + round256(msf::kCacheMaxCtas * 4) +
+                        round256(msf::kCachePartialFloats * 4);
+    *out = c;
+    return MSF_OK;
+}
+
+extern "C" void msf_cache_destroy(msf_cache_t cache) { delete cache; }
+
+extern "C" msf_status msf_cache_query(msf_cache_t cache, msf_cache_info* info) {
+    if (!cache || !info) return MSF_ERR_INVALID_ARG;
+    *info = cache->info;
+    return MSF_OK;
+}
+
+extern "C" msf_status msf_cache_bind(msf_cache_t cache, void* pool, size_t pool_bytes, void* state, size_t state_bytes,
+                                     void* workspace, size_t workspace_bytes) {
+    if (!cache || !pool || !state || !workspace) return MSF_ERR_INVALID_ARG;
+    if (!aligned16(pool) || !aligned16(state) || !aligned16(workspace)) return MSF_ERR_INVALID_ARG;
+    const msf_cache_info& i = cache->info;
+    if (pool_bytes < i.pool_bytes || state_bytes < i.state_bytes || workspace_bytes < i.workspace_bytes)
+        return MSF_ERR_WORKSPACE;
+    CacheView& v = cache->v;
+    using msf::round256;
+    char* s = (char*)state;
+    v.pool = (uint8_t*)pool;
+    v.head = (unsigned*)s;
+    v.lengths = (int*)(s + i.lengths_offset);
+    v.table = (int*)(s + i.table_offset);
+    v.refs = (int*)(s + i.refs_offset);
+    v.used = (unsigned*)(s + i.refs_offset + round256((size_t)v.pages * 4));
+    char* w = (char*)workspace;
+    auto take = [&w](size_t bytes) {
+        char* p = w;
+        w += round256(bytes);
+        return p;
+    };
+    v.claim = (int*)take((size_t)v.S * 4);
+    v.row = (int*)take((size_t)v.S * 4);
+    v.new_len = (int*)take((size_t)v.S * 4);
+    v.free_list = (int*)take((size_t)v.pages * 4);
+    v.moved = (int*)take((size_t)v.pages * 4);
+    v.copies = (int2*)take((size_t)v.pages * 8);
+    v.stage = (int*)take((size_t)v.S * v.W * 4);
+    v.counters = (unsigned*)take(msf::kCacheMaxCtas * 4);
+    v.partials = (float*)take(msf::kCachePartialFloats * 4);
+    cache->bound = false;
+    cudaError_t e = cudaMemset(state, 0, i.state_bytes);
+    if (e == cudaSuccess) e = cudaMemset(v.table, 0xff, (size_t)v.S * v.W * 4);
+    if (e == cudaSuccess) e = cudaMemset(v.counters, 0, msf::kCacheMaxCtas * 4);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    cache->bound = e == cudaSuccess;
+    return cuda_status(e);
+}
+
+extern "C" msf_status msf_cache_grow(msf_cache_t cache, const int32_t* seqs, const int32_t* counts, int32_t tokens,
+                                     int32_t n, void* stream) {
+    if (!cache) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    if (!list_ok(cache, n, seqs, counts) || tokens < 0) return MSF_ERR_INVALID_ARG;
+    if (n == 0) return MSF_OK;
+    return cuda_status(msf::launch_cache_grow(cache->v, seqs, counts, tokens, n, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_write(msf_cache_t cache, int32_t layer, const int32_t* seqs, const int32_t* counts,
+                                      int32_t n, int32_t tokens, const void* k, const void* v, const int64_t strides[3],
+                                      void* stream) {
+    const msf_status st = rows_check(cache, layer, seqs, counts, n, tokens, k, v, strides);
+    if (st != MSF_OK || n == 0 || tokens == 0) return st;
+    return cuda_status(msf::launch_cache_write(cache->v, rows_of(layer, seqs, counts, n, tokens, strides),
+                                               (const uint16_t*)k, (const uint16_t*)v, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_read(msf_cache_t cache, int32_t layer, const int32_t* seqs, const int32_t* begins,
+                                     int32_t n, int32_t tokens, void* k, void* v, const int64_t strides[3], void* stream) {
+    const msf_status st = rows_check(cache, layer, seqs, begins, n, tokens, k, v, strides);
+    if (st != MSF_OK || n == 0 || tokens == 0) return st;
+    return cuda_status(msf::launch_cache_read(cache->v, rows_of(layer, seqs, begins, n, tokens, strides), (uint16_t*)k,
+                                              (uint16_t*)v, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_fork(msf_cache_t cache, const int32_t* src, const int32_t* dst, const int32_t* lengths,
+                                     int32_t n, int32_t flags, void* stream) {
+    if (!cache) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    if (!list_ok(cache, n, src, dst) || !aligned4(lengths)) return MSF_ERR_INVALID_ARG;
+    if (flags != MSF_CACHE_FORK_SHARE && flags != MSF_CACHE_FORK_COPY) return MSF_ERR_INVALID_ARG;
+    if (n == 0) return MSF_OK;
+    if (!src || !dst) return MSF_ERR_INVALID_ARG;
+    return cuda_status(msf::launch_cache_fork(cache->v, src, dst, lengths, n, flags == MSF_CACHE_FORK_COPY,
+                                              (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_truncate(msf_cache_t cache, const int32_t* seqs, const int32_t* lengths, int32_t n,
+                                         void* stream) {
+    if (!cache) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    if (!list_ok(cache, n, seqs, lengths)) return MSF_ERR_INVALID_ARG;
+    if (n == 0) return MSF_OK;
+    return cuda_status(msf::launch_cache_truncate(cache->v, seqs, lengths, n, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_compact(msf_cache_t cache, void* stream) {
+    if (!cache) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    return cuda_status(msf::launch_cache_compact(cache->v, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                                       const msf_cache_attention* args, void* stream) {
+    if (!cache || !args || layer < 0 || layer >= cache->d.layers) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    const msf_cache_attention& x = *args;
+    // seqs may repeat here, so n is not bounded by the cache's sequences, unless it stands for 0..n-1
+    if (n < 0 || (!seqs && n > cache->d.sequences) || !aligned4(seqs)) return MSF_ERR_INVALID_ARG;
+    if (x.queries < 0 || x.heads < 1 || x.heads % cache->d.kv_heads) return MSF_ERR_INVALID_ARG;
+    if (x.causal != 0 && x.causal != 1) return MSF_ERR_INVALID_ARG;
+    if (!(x.softmax_scale >= 0.f) || !isfinite(x.softmax_scale)) return MSF_ERR_INVALID_ARG;
+    if (!strides_ok(x.q_strides) || !strides_ok(x.out_strides)) return MSF_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+        if (x.lse_strides[i] < 0 || x.lse_strides[i] > (int64_t)1 << 40) return MSF_ERR_INVALID_ARG;
+    if (n == 0 || x.queries == 0) return MSF_OK;
+    if (!x.q || !x.out || !aligned16(x.q) || !aligned16(x.out)) return MSF_ERR_INVALID_ARG;
+    if ((x.base_out == nullptr) != (x.base_lse == nullptr)) return MSF_ERR_INVALID_ARG;
+    if (!aligned16(x.base_out) || !aligned4(x.base_lse) || !aligned4(x.lse)) return MSF_ERR_INVALID_ARG;
+    if ((double)n * x.heads * x.queries >= 2147483648.0) return MSF_ERR_UNSUPPORTED;
+    msf::CacheAttnArgs a;
+    a.q = (const uint16_t*)x.q;
+    a.out = (uint16_t*)x.out;
+    a.lse = x.lse;
+    a.base_out = (const uint16_t*)x.base_out;
+    a.base_lse = x.base_lse;
+    for (int i = 0; i < 3; ++i) {
+        a.q_st[i] = x.q_strides[i];
+        a.o_st[i] = x.out_strides[i];
+    }
+    a.l_st[0] = x.lse_strides[0];
+    a.l_st[1] = x.lse_strides[1];
+    a.queries = x.queries;
+    a.heads = x.heads;
+    a.group = x.heads / cache->d.kv_heads;
+    a.causal = x.causal;
+    a.layer = layer;
+    a.n = n;
+    a.seqs = seqs;
+    a.scale = x.softmax_scale > 0.f ? x.softmax_scale : 1.0f / sqrtf((float)cache->d.head_dim);
+    return cuda_status(msf::launch_cache_attend(cache->v, a, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_device_status(msf_cache_t cache, void* stream) {
+    if (!cache) return MSF_ERR_INVALID_ARG;
+    if (!cache->bound) return MSF_ERR_STATE;
+    const CacheView& v = cache->v;
+    cudaStream_t s = (cudaStream_t)stream;
+    unsigned word = 0;
+    cudaError_t e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&word, v.head + msf::kCacheStatus, sizeof(word), cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaMemsetAsync(v.head, 0, sizeof(word), s);
+    // An attention that gave up may have left pieces counted.
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess && (word & msf::kDevTimeout)) {
+        e = cudaMemsetAsync(v.counters, 0, msf::kCacheMaxCtas * 4, s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    }
+    if (e != cudaSuccess) return cuda_status(e);
+    if (word & msf::kDevTimeout) return MSF_ERR_TIMEOUT;
+    if (word & msf::kDevPages) return MSF_ERR_PAGES;
+    if (word & msf::kDevIndex) return MSF_ERR_INVALID_ARG;
+    if (word & msf::kDevNonfinite) return MSF_ERR_NONFINITE;
+    return MSF_OK;
+}

@@ -30,6 +30,8 @@ extern "C" const char* msf_status_string(msf_status s) {
         case MSF_ERR_TIMEOUT: return "device wait timed out";
         case MSF_ERR_STATE: return "invalid plan state";
         case MSF_ERR_WORKSPACE: return "workspace too small";
+        case MSF_ERR_PAGES: return "no cache pages left";
+        case MSF_ERR_NONFINITE: return "appended values were not finite";
     }
     return "unknown status";
 }

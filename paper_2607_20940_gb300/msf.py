@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libmsf.so (include/msf.h).
+"""Thin ctypes binding of libmsf.so (include/msf.h, include/msf_cache.h).
 
 Argument marshalling only: every step of the window pass runs in the CUDA
 kernels behind the C ABI. Tensors are passed by device pointer; torch is used
@@ -21,12 +21,16 @@ MSF_ERR_CUDA = 3
 MSF_ERR_TIMEOUT = 4
 MSF_ERR_STATE = 5
 MSF_ERR_WORKSPACE = 6
+MSF_ERR_PAGES = 7
+MSF_ERR_NONFINITE = 8
 MSF_DTYPE_BF16 = 0
 MSF_DTYPE_F32 = 1
 MSF_RESAMPLE_AVG = 0
 MSF_RESAMPLE_STRIDED = 1
 MSF_RESAMPLE_FULL = 0
 MSF_RESAMPLE_WINDOW_ONLY = 1
+MSF_CACHE_FORK_SHARE = 0
+MSF_CACHE_FORK_COPY = 1
 MSF_MAX_STATES = 16
 MSF_MAX_GROUPS = 8
 
@@ -39,6 +43,9 @@ EXPORTS = (
     "msf_mssa_backward", "msf_mssa_backward_simt", "msf_history_get", "msf_history_set",
     "msf_noalloc_device_status", "msf_noalloc_selftest_wait_timeout", "msf_patchify_tiers",
     "msf_unpatchify_tier", "msf_patchify_resample", "msf_mssa_forward_resample",
+    "msf_cache_create", "msf_cache_destroy", "msf_cache_query", "msf_cache_bind", "msf_cache_grow",
+    "msf_cache_write", "msf_cache_read", "msf_cache_fork", "msf_cache_truncate", "msf_cache_compact",
+    "msf_cache_attend", "msf_cache_device_status",
 )
 
 
@@ -91,11 +98,34 @@ class msf_plan_info(ctypes.Structure):
     ]
 
 
+class msf_cache_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("layers", "kv_heads", "head_dim", "page_tokens", "pages", "sequences", "sequence_pages",
+                 "k_exponent", "v_exponent")]
+
+
+class msf_cache_info(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint64) for n in
+                ("pool_bytes", "page_bytes", "state_bytes", "workspace_bytes", "lengths_offset",
+                 "table_offset", "refs_offset")]
+
+
+class msf_cache_attention(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("base_out", ctypes.c_void_p), ("base_lse", ctypes.c_void_p),
+        ("q_strides", ctypes.c_int64 * 3), ("out_strides", ctypes.c_int64 * 3),
+        ("lse_strides", ctypes.c_int64 * 2), ("queries", ctypes.c_int32), ("heads", ctypes.c_int32),
+        ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+    ]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: run __graft_entry__.build() first")
     lib = ctypes.CDLL(LIB_PATH)
     P, VP, I32, SZ = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    I64P = ctypes.POINTER(ctypes.c_int64)
     sig = {
         "msf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "msf_last_cuda_error": (ctypes.c_int, []),
@@ -128,6 +158,18 @@ def _load():
         "msf_mssa_forward_lse": (ctypes.c_int, [P, VP, VP, VP, VP, VP, VP]),
         "msf_mssa_backward": (ctypes.c_int, [P, VP, VP, VP, VP, VP, VP, VP, VP, VP, VP, SZ, VP]),
         "msf_mssa_backward_simt": (ctypes.c_int, [P, VP, VP, VP, VP, VP, VP, VP, VP, VP, VP, SZ, VP]),
+        "msf_cache_create": (ctypes.c_int, [ctypes.POINTER(msf_cache_desc), ctypes.POINTER(P)]),
+        "msf_cache_destroy": (None, [P]),
+        "msf_cache_query": (ctypes.c_int, [P, ctypes.POINTER(msf_cache_info)]),
+        "msf_cache_bind": (ctypes.c_int, [P, VP, SZ, VP, SZ, VP, SZ]),
+        "msf_cache_grow": (ctypes.c_int, [P, VP, VP, I32, I32, VP]),
+        "msf_cache_write": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, I64P, VP]),
+        "msf_cache_read": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, I64P, VP]),
+        "msf_cache_fork": (ctypes.c_int, [P, VP, VP, VP, I32, I32, VP]),
+        "msf_cache_truncate": (ctypes.c_int, [P, VP, VP, I32, VP]),
+        "msf_cache_compact": (ctypes.c_int, [P, VP]),
+        "msf_cache_attend": (ctypes.c_int, [P, I32, VP, I32, ctypes.POINTER(msf_cache_attention), VP]),
+        "msf_cache_device_status": (ctypes.c_int, [P, VP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -353,7 +395,108 @@ def msf_kernel_launches() -> int:
     return int(_lib.msf_kernel_launches())
 
 
+# The cache (msf_cache.h). Tensors of rows are torch tensors, whose strides are
+# passed on; lists are int32 device tensors.
+
+def _list(t, n=None):
+    """An int32 device list (or None) and its length."""
+    if t is None:
+        return None, n
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("a list is a contiguous one-dimensional int32 tensor on the device")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"a list has {t.numel()} entries where {n} are wanted")
+    return t.data_ptr(), t.numel()
+
+
+def _rows(t, dtype, name, shape=None):
+    """Strides (elements) of a tensor of rows whose last dimension is contiguous."""
+    if t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: a {dtype} tensor on the device is wanted")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, where {tuple(shape)} is wanted")
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension has to be contiguous")
+    # the stride of a dimension of one is anything
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+
+
+def msf_cache_create(desc: msf_cache_desc) -> int:
+    h = ctypes.c_void_p()
+    _check(_lib.msf_cache_create(ctypes.byref(desc), ctypes.byref(h)), "msf_cache_create")
+    return h.value
+
+
+def msf_cache_destroy(cache: int) -> None:
+    _lib.msf_cache_destroy(cache)
+
+
+def msf_cache_query(cache: int) -> msf_cache_info:
+    info = msf_cache_info()
+    _check(_lib.msf_cache_query(cache, ctypes.byref(info)), "msf_cache_query")
+    return info
+
+
+def msf_cache_bind(cache: int, pool, state, workspace) -> None:
+    size = lambda t: t.numel() * t.element_size()  # noqa: E731
+    _check(_lib.msf_cache_bind(cache, _ptr(pool), size(pool), _ptr(state), size(state), _ptr(workspace),
+                               size(workspace)), "msf_cache_bind")
+
+
+def msf_cache_grow(cache: int, seqs, counts, tokens: int, n: int, stream=None) -> None:
+    _check(_lib.msf_cache_grow(cache, seqs, counts, tokens, n, _stream(stream)), "msf_cache_grow")
+
+
+def _row_call(fn, where, cache, layer, k, v, seqs, at, stream):
+    import torch
+    if k.dim() != 4:
+        raise ValueError(f"{where}: k and v are [rows, tokens, kv_heads, head_dim]")
+    strides = _rows(k, torch.bfloat16, "k")
+    if _rows(v, torch.bfloat16, "v", k.shape) != strides:
+        raise ValueError(f"{where}: k and v have the same strides")
+    n = k.shape[0]
+    _check(fn(cache, layer, _list(seqs, n)[0], _list(at, n)[0], n, k.shape[1], _ptr(k), _ptr(v),
+              (ctypes.c_int64 * 3)(*strides), _stream(stream)), where)
+
+
+def msf_cache_write(cache: int, layer: int, k, v, seqs=None, counts=None, stream=None) -> None:
+    _row_call(_lib.msf_cache_write, "msf_cache_write", cache, layer, k, v, seqs, counts, stream)
+
+
+def msf_cache_read(cache: int, layer: int, k, v, seqs=None, begins=None, stream=None) -> None:
+    _row_call(_lib.msf_cache_read, "msf_cache_read", cache, layer, k, v, seqs, begins, stream)
+
+
+def msf_cache_fork(cache: int, src, dst, lengths=None, flags: int = MSF_CACHE_FORK_SHARE, stream=None) -> None:
+    p, n = _list(src)
+    _check(_lib.msf_cache_fork(cache, p, _list(dst, n)[0], _list(lengths, n)[0], n, flags, _stream(stream)),
+           "msf_cache_fork")
+
+
+def msf_cache_truncate(cache: int, seqs, lengths, n: int, stream=None) -> None:
+    _check(_lib.msf_cache_truncate(cache, seqs, lengths, n, _stream(stream)), "msf_cache_truncate")
+
+
+def msf_cache_compact(cache: int, stream=None) -> None:
+    _check(_lib.msf_cache_compact(cache, _stream(stream)), "msf_cache_compact")
+
+
+def msf_cache_attend(cache: int, layer: int, seqs, n: int, args: msf_cache_attention, stream=None) -> None:
+    _check(_lib.msf_cache_attend(cache, layer, seqs, n, ctypes.byref(args), _stream(stream)), "msf_cache_attend")
+
+
+def msf_cache_device_status(cache: int, stream=None) -> int:
+    return _lib.msf_cache_device_status(cache, _stream(stream))
+
+
 # ------------------------------------------------------------ convenience
+
+def make_cache_desc(layers, kv_heads, head_dim, page_tokens, pages, sequences, sequence_pages, k_exponent=0,
+                    v_exponent=0) -> msf_cache_desc:
+    return msf_cache_desc(layers, kv_heads, head_dim, page_tokens, pages, sequences, sequence_pages, k_exponent,
+                          v_exponent)
+
 
 def make_desc(scales, grid_h, grid_w, heads, head_dim, sink_tokens, history_frames,
               history_capacity=None, batch=1, dtype=MSF_DTYPE_BF16, resample=MSF_RESAMPLE_AVG,
@@ -474,3 +617,132 @@ class Plan:
 
     def selftest_wait_timeout(self, limit_cycles, stream=None):
         msf_selftest_wait_timeout(self.handle, limit_cycles, stream)
+
+
+class Cache:
+    """Owns a cache handle and the device buffers bound to it (torch tensors).
+
+    Lists (`seqs`, `counts`, ...) are int32 device tensors; `seqs` None stands for the
+    sequences 0, 1, ... in order."""
+
+    def __init__(self, desc: msf_cache_desc):
+        self.desc = desc
+        self.handle = msf_cache_create(desc)
+        self.info = msf_cache_query(self.handle)
+        self.bound_pool = self.bound_state = self.bound_workspace = None
+
+    def close(self):
+        if self.handle:
+            msf_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _buffer(self, nbytes, device):
+        import torch
+        return torch.empty(int(nbytes), dtype=torch.uint8, device=device)
+
+    def pool(self, device="cuda"):
+        return self._buffer(self.info.pool_bytes, device)
+
+    def state(self, device="cuda"):
+        return self._buffer(self.info.state_bytes, device)
+
+    def workspace(self, device="cuda"):
+        return self._buffer(self.info.workspace_bytes, device)
+
+    def bind(self, pool, state, workspace):
+        msf_cache_bind(self.handle, pool, state, workspace)
+        self.bound_pool, self.bound_state, self.bound_workspace = pool, state, workspace
+
+    def _ints(self, offset, n):
+        import torch
+        return self.bound_state[int(offset):int(offset) + 4 * n].view(torch.int32)
+
+    @property
+    def lengths(self):
+        """Tokens of each sequence: a view of the state."""
+        return self._ints(self.info.lengths_offset, self.desc.sequences)
+
+    @property
+    def table(self):
+        """Pages of each sequence, -1 past its last: a view of the state."""
+        d = self.desc
+        return self._ints(self.info.table_offset, d.sequences * d.sequence_pages).view(d.sequences, d.sequence_pages)
+
+    @property
+    def refs(self):
+        """Tables that name each page, 0 for a free one: a view of the state."""
+        return self._ints(self.info.refs_offset, self.desc.pages)
+
+    def grow(self, seqs=None, counts=None, tokens=0, stream=None):
+        """Room for counts[i] (or `tokens`) more tokens of each listed sequence."""
+        n = self.desc.sequences
+        if seqs is not None:
+            n = seqs.numel()
+        elif counts is not None:
+            n = counts.numel()
+        msf_cache_grow(self.handle, _list(seqs, n)[0], _list(counts, n)[0], tokens, n, stream)
+
+    def write(self, layer, k, v, seqs=None, counts=None, stream=None):
+        """Quantise the newest tokens: k, v bf16 [rows, tokens, kv_heads, head_dim]."""
+        self._heads(k, v)
+        msf_cache_write(self.handle, layer, k, v, seqs, counts, stream)
+
+    def read(self, layer, k, v, seqs=None, begins=None, stream=None):
+        """Read tokens from begins[i] on (0) back into bf16 k, v."""
+        self._heads(k, v)
+        msf_cache_read(self.handle, layer, k, v, seqs, begins, stream)
+
+    def _heads(self, *rows):
+        for t in rows:
+            if tuple(t.shape[-2:]) != (self.desc.kv_heads, self.desc.head_dim):
+                raise ValueError(f"rows of {tuple(t.shape[-2:])} heads, where the cache holds "
+                                 f"{(self.desc.kv_heads, self.desc.head_dim)}")
+
+    def fork(self, src, dst, lengths=None, copy=False, stream=None):
+        """dst[i] becomes (the first lengths[i] tokens of) src[i], sharing its pages or with copies of them."""
+        msf_cache_fork(self.handle, src, dst, lengths, MSF_CACHE_FORK_COPY if copy else MSF_CACHE_FORK_SHARE, stream)
+
+    def truncate(self, seqs=None, lengths=None, stream=None):
+        """Keep the first lengths[i] tokens (none) of each listed sequence."""
+        n = self.desc.sequences
+        if seqs is not None:
+            n = seqs.numel()
+        elif lengths is not None:
+            n = lengths.numel()
+        msf_cache_truncate(self.handle, _list(seqs, n)[0], _list(lengths, n)[0], n, stream)
+
+    def compact(self, stream=None):
+        """Move the pages in use to the lowest numbers."""
+        msf_cache_compact(self.handle, stream)
+
+    def attend(self, layer, q, out, lse=None, base_out=None, base_lse=None, seqs=None, causal=False,
+               softmax_scale=0.0, stream=None):
+        """Attention of q [rows, queries, heads, head_dim] over the listed sequences, joined with
+        (base_out, base_lse) where given; lse [rows, heads, queries]."""
+        import torch
+        if q.dim() != 4 or q.shape[3] != self.desc.head_dim:
+            raise ValueError(f"q is [rows, queries, heads, {self.desc.head_dim}]")
+        a = msf_cache_attention()
+        a.q, a.out, a.lse, a.base_out, a.base_lse = _ptr(q), _ptr(out), _ptr(lse), _ptr(base_out), _ptr(base_lse)
+        a.q_strides[:] = _rows(q, torch.bfloat16, "q")
+        a.out_strides[:] = _rows(out, torch.bfloat16, "out", q.shape)
+        if base_out is not None and _rows(base_out, torch.bfloat16, "base_out", q.shape) != list(a.out_strides):
+            raise ValueError("base_out and out have the same strides")
+        n, queries, heads, _ = q.shape
+        for t, name in ((lse, "lse"), (base_lse, "base_lse")):
+            if t is not None:
+                strides = _rows(t, torch.float32, name, (n, heads, queries))
+                if name == "base_lse" and lse is not None and strides != list(a.lse_strides):
+                    raise ValueError("base_lse and lse have the same strides")
+                a.lse_strides[:] = strides
+        a.queries, a.heads, a.causal, a.softmax_scale = queries, heads, int(causal), softmax_scale
+        msf_cache_attend(self.handle, layer, _list(seqs, n)[0], n, a, stream)
+
+    def device_status(self, stream=None) -> int:
+        return msf_cache_device_status(self.handle, stream)
