@@ -164,6 +164,13 @@ typedef struct msf_cache_attention {
 msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
                             const msf_cache_attention* args, void* stream);
 
+/* The same on fp32 CUDA cores, as msf_mssa_forward_simt is to msf_mssa_forward:
+ * the check of msf_cache_attend's tensor-core kernels, and the form for whom
+ * their probabilities are too coarse (in f16: 11 bits down to 2^-19 of a row's
+ * largest, multiples of at most 2^-29 of it below). */
+msf_status msf_cache_attend_simt(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                                 const msf_cache_attention* args, void* stream);
+
 /* Synchronise `stream`, read and clear the device status. In order of weight:
  * TIMEOUT (a bounded wait gave up), PAGES (no page or table entry left),
  * INVALID_ARG (a list named a sequence that is none, one twice, or a negative

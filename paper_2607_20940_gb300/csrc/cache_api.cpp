@@ -206,8 +206,8 @@ extern "C" msf_status msf_cache_compact(msf_cache_t cache, void* stream) {
     return cuda_status(msf::launch_cache_compact(cache->v, (cudaStream_t)stream));
 }
 
-extern "C" msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
-                                       const msf_cache_attention* args, void* stream) {
+static msf_status attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                         const msf_cache_attention* args, void* stream, bool simt) {
     if (!cache || !args || layer < 0 || layer >= cache->d.layers) return MSF_ERR_INVALID_ARG;
     if (!cache->bound) return MSF_ERR_STATE;
     const msf_cache_attention& x = *args;
@@ -244,7 +244,18 @@ extern "C" msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const i
     a.n = n;
     a.seqs = seqs;
     a.scale = x.softmax_scale > 0.f ? x.softmax_scale : 1.0f / sqrtf((float)cache->d.head_dim);
-    return cuda_status(msf::launch_cache_attend(cache->v, a, (cudaStream_t)stream));
+    return cuda_status(simt ? msf::launch_cache_attend_simt(cache->v, a, (cudaStream_t)stream)
+                            : msf::launch_cache_attend(cache->v, a, (cudaStream_t)stream));
+}
+
+extern "C" msf_status msf_cache_attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                                       const msf_cache_attention* args, void* stream) {
+    return attend(cache, layer, seqs, n, args, stream, false);
+}
+
+extern "C" msf_status msf_cache_attend_simt(msf_cache_t cache, int32_t layer, const int32_t* seqs, int32_t n,
+                                            const msf_cache_attention* args, void* stream) {
+    return attend(cache, layer, seqs, n, args, stream, true);
 }
 
 extern "C" msf_status msf_cache_device_status(msf_cache_t cache, void* stream) {

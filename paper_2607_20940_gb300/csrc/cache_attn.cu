@@ -1,9 +1,9 @@
-// Attention over the 4-bit cache on CUDA cores: a block per (sequence, query,
-// head), its four warps over the tokens, in fp32 throughout.
+// Attention over the 4-bit cache.
 #include <cuda_runtime.h>
 #include <math.h>
 
 #include "cache.h"
+#include "cache_codes.cuh"
 #include "internal.h"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -28,6 +28,9 @@ __device__ __forceinline__ float2 e2m1_f(uint32_t byte) {
 }
 __device__ __forceinline__ float bf(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
+// The check of the kernels below, in fp32 throughout on CUDA cores: a block per
+// (sequence, query, head), its four warps over the tokens.
+//
 // Lanes hold neighbouring pairs of the head: D / 64 pairs each, 64 apart.
 template <int D>
 __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, const CacheAttnArgs a) {
@@ -129,12 +132,542 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
     }
 }
 
+// ------------------------------------------------------------- few queries
+//
+// Up to 8 NT rows (the queries of the heads that share a key head) against a
+// sequence's tokens: bound by HBM (9/8 D bytes a token and key head, 4 D NT 8
+// operations). A warp takes a record of 16 tokens at a time:
+//   scores [16 tokens x 8 rows] += K [16 x 16] Q^T, D / 16 products,
+//   out^T [16 dims x 8 rows] += V^T [16 x 16 tokens] P^T, D / 16 products,
+// mma.sync products of f16 in fp32: tcgen05 would need 64 rows, and the codes
+// would have to pass through shared memory. A code times its scale is exact in
+// f16. Which of a product's 16 columns stands for which dim or token is free,
+// so each lane keeps what it loads: 32 neighbouring dims of two tokens for the
+// scores, one block of four neighbouring tokens for the outputs, in whole
+// 64-byte rows per four and eight lanes. Two records are in flight per warp.
+//
+// Work: every (sequence, key head) is cut into steps of 128 tokens (a record for
+// each of the eight warps); the CTAs take equal, contiguous shares of all steps.
+// A piece that is not a whole (sequence, head) leaves its unnormalised output,
+// maximum and sum in a slot, and the last CTA of it to finish adds the pieces in
+// order (the same bits whichever is last).
+
+constexpr int kWarps = 8;
+constexpr int kStep = 16 * kWarps;  // tokens
+constexpr float kLowest = -3.402823466e38f;
+
+// c += a b, f16 in fp32.
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+// What a lane holds of a record: lane 4 g + t.
+template <int D>
+struct Record {
+    uint32_t k[2][D / 32];  // tokens 4 (g / 2) + g % 2 and + 2: dims D / 4 t ...
+    uint32_t ks[2];         // and their scales
+    uint32_t v[4][D / 64];  // tokens 4 t ...: dims D / 8 g ...
+    uint32_t vs;            // and their four scales
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&d)[N], const uint8_t* p) {
+    if constexpr (N == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        d[0] = x.x, d[1] = x.y, d[2] = x.z, d[3] = x.w;
+    } else if constexpr (N == 2) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        d[0] = x.x, d[1] = x.y;
+    } else {
+        d[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void load_record(Record<D>& r, const uint8_t* rec, int g, int t) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int tok = 4 * (g / 2) + g % 2 + 2 * e;
+        load_words(r.k[e], rec + tok * (D / 2) + t * (D / 8));
+        const uint8_t* s = rec + cache_k_scales(D) + tok * (D / 16) + t * (D / 64);
+        if constexpr (D == 128)
+            r.ks[e] = *reinterpret_cast<const uint16_t*>(s);
+        else
+            r.ks[e] = *s;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) load_words(r.v[e], rec + cache_v_codes(D) + (4 * t + e) * (D / 2) + g * (D / 16));
+    r.vs = *reinterpret_cast<const uint32_t*>(rec + cache_v_scales(D) + (D == 128 ? g : g / 2) * 16 + 4 * t);
+}
+
+// Byte J of four words as the product's f16 operand, times scales.
+template <int J>
+__device__ __forceinline__ void operand(uint32_t (&a)[4], uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t s0,
+                                        uint32_t s1, uint32_t s2, uint32_t s3) {
+    a[0] = codes::mul_f16x2(codes::e2m1_f16x2<J>(w0), s0);
+    a[1] = codes::mul_f16x2(codes::e2m1_f16x2<J>(w1), s1);
+    a[2] = codes::mul_f16x2(codes::e2m1_f16x2<J>(w2), s2);
+    a[3] = codes::mul_f16x2(codes::e2m1_f16x2<J>(w3), s3);
+}
+
+template <int D, int NT>
+struct FewCfg {
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kPitch = D + 4;  // floats of a row of outputs in shared memory
+    static constexpr int kSmem = kWarps * kRows * kPitch * 4;
+    static constexpr int kSlot = kRows * (D + 2);  // floats of a piece's partial result
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
+    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_steps) {
+    using C = FewCfg<D, NT>;
+    constexpr int kT = 32 * kWarps;
+    extern __shared__ __align__(16) float so[];  // [warp][row][kPitch]
+    __shared__ float sm[kWarps][C::kRows], sl[kWarps][C::kRows];
+    __shared__ float sw[kWarps][C::kRows], s_own[C::kRows], s_other[C::kRows], sM[C::kRows], sL[C::kRows];
+    __shared__ long long s_scan[kWarps];
+    __shared__ long long s_found[2];
+    __shared__ int s_last;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const int rows = a.group * a.queries;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+
+    auto length = [&](int i) -> int {
+        const int s = a.seqs ? a.seqs[i] : i;
+        return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
+    };
+    auto steps_of = [&](int len) { return (len + kStep - 1) / kStep; };
+    // Row r of (sequence i, key head hk): its place in q, out and lse.
+    auto place = [&](const long long* st, int i, int hk, int r) {
+        return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
+    };
+    auto lse_place = [&](int i, int hk, int r) {
+        return i * a.l_st[0] + (hk * a.group + r % a.group) * a.l_st[1] + r / a.group;
+    };
+    // Sum of `x` over the block's threads before this one; all: over all.
+    auto scan = [&](long long x, long long& all) {
+        long long v = x;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const long long y = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += y;
+        }
+        if (lane == 31) s_scan[warp] = v;
+        __syncthreads();
+        long long before = 0;
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += s_scan[w];
+            all += s_scan[w];
+        }
+        __syncthreads();
+        return before + v - x;
+    };
+
+    // ---- sequences without tokens: their rows are empty, or the base's
+    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk; x += gridDim.x) {
+        const int i = (int)(x / c.Hk), hk = (int)(x % c.Hk);
+        if (length(i) > 0) continue;
+        if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
+        for (int y = threadIdx.x; y < rows * (D / 8); y += kT) {
+            const int r = y / (D / 8), d = y % (D / 8) * 8;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
+                w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
+            *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+        }
+        if (a.lse && a.lse != a.base_lse)
+            for (int r = threadIdx.x; r < rows; r += kT)
+                a.lse[lse_place(i, hk, r)] = a.base_lse ? a.base_lse[lse_place(i, hk, r)] : -INFINITY;
+    }
+
+    // ---- this CTA's share of the steps, and the (sequence, head) it begins in
+    long long U = 0, mine = 0;
+    for (int i = threadIdx.x; i < a.n; i += kT) mine += steps_of(length(i));
+    scan(mine, U);
+    U *= c.Hk;
+    const int G = (int)min((long long)gridDim.x, max(1ll, U / min_steps));
+    if ((int)blockIdx.x >= G) return;
+    const long long u0 = U * blockIdx.x / G, u1 = U * (blockIdx.x + 1) / G;
+    if (u0 >= u1) return;
+    auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
+    long long base = 0;
+    for (int i0 = 0; i0 < a.n; i0 += kT) {
+        const int i = i0 + (int)threadIdx.x;
+        const long long x = i < a.n ? (long long)steps_of(length(i)) * c.Hk : 0;
+        long long all;
+        const long long before = base + scan(x, all);
+        if (u0 >= before && u0 < before + x) {
+            s_found[0] = i;
+            s_found[1] = before;
+        }
+        base += all;
+        if (u0 < base) break;
+    }
+    __syncthreads();
+    int seq = (int)s_found[0];
+    long long seq0 = s_found[1];  // first step of the sequence
+
+    for (long long u = u0; u < u1;) {
+        const int len = length(seq), n_steps = steps_of(len);
+        if (u >= seq0 + (long long)n_steps * c.Hk) {
+            seq0 += (long long)n_steps * c.Hk;
+            ++seq;
+            continue;
+        }
+        const int hk = (int)((u - seq0) / n_steps);
+        const long long item0 = seq0 + (long long)hk * n_steps;
+        const int b0 = (int)(u - item0), b1 = (int)min((long long)n_steps, u1 - item0);
+        u = item0 + b1;
+        const int r_end = min((len + 15) / 16, b1 * kWarps);
+        const int* row = c.table + (size_t)(a.seqs ? a.seqs[seq] : seq) * c.W;
+        const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes +
+                              (long long)hk * (c.P / 16) * cache_record_bytes(D);
+        auto page_of = [&](int r) { return row[r >> (c.log2_p - 4)]; };
+        auto fetch = [&](Record<D>& x, int r, int page) {
+            // a page number from outside is read as page 0, like any stale page
+            const long long at = cache_page_ok(c, page) ? page : 0;
+            load_record<D>(x, pool + at * c.page_bytes + (r & (c.P / 16 - 1)) * cache_record_bytes(D), g, t);
+        };
+        Record<D> rec[2];
+        int r0 = b0 * kWarps + warp;
+        int page_next = 0;
+        if (r0 < r_end) fetch(rec[0], r0, page_of(r0));
+        if (r0 + kWarps < r_end) fetch(rec[1], r0 + kWarps, page_of(r0 + kWarps));
+        if (r0 + 2 * kWarps < r_end) page_next = page_of(r0 + 2 * kWarps);
+
+        // ---- queries: row g + 8 nt, dims D / 4 t ...
+        uint32_t qf[NT][D / 16][2];
+        float f[NT][2];  // of rows 2 t and 2 t + 1: to base-2 scores
+        int limit[NT][2];  // tokens that they see
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = 8 * nt + g;
+            uint32_t w[D / 8];
+            if (r < rows) {
+                const uint16_t* q = a.q + place(a.q_st, seq, hk, r) + t * (D / 4);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(q + 8 * e);
+                    w[4 * e] = x.x, w[4 * e + 1] = x.y, w[4 * e + 2] = x.z, w[4 * e + 3] = x.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < D / 8; ++e) w[e] = 0u;
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < D / 8; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = codes::row_exponent(top);
+            const float up = codes::row_up(e);
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t y = w[2 * m + x];
+                    qf[nt][m][x] = codes::pack_f16(codes::bf(y & 0xffffu) * up, __uint_as_float(y & 0xffff0000u) * up);
+                }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                f[nt][x] = codes::row_down(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x))) * (a.scale * c.k_unit) *
+                           1.4426950408889634f;
+                const int rr = 8 * nt + 2 * t + x;
+                limit[nt][x] = rr >= rows ? 0 : a.causal ? len - a.queries + 1 + rr / a.group : len;
+            }
+        }
+        // no record below this one hides a token from a row
+        const int all_see = a.causal ? max(0, len - a.queries + 1) : len;
+
+        float o[NT][D / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = kLowest;
+            l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+        }
+        auto work = [&](Record<D>& x, int r) {
+            float s[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+            {
+                const uint32_t k0 = codes::e4m3_f16x2(x.ks[0]), k1 = codes::e4m3_f16x2(x.ks[1]);
+                auto part = [&](int wi, uint32_t s0, uint32_t s1) {  // words wi and wi + 1: a block of 16 dims
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t w0 = x.k[0][wi + e], w1 = x.k[1][wi + e];
+                        uint32_t op[4];
+                        op[0] = codes::mul_f16x2(codes::e2m1_f16x2<0>(w0), s0);
+                        op[1] = codes::mul_f16x2(codes::e2m1_f16x2<0>(w1), s1);
+                        op[2] = codes::mul_f16x2(codes::e2m1_f16x2<1>(w0), s0);
+                        op[3] = codes::mul_f16x2(codes::e2m1_f16x2<1>(w1), s1);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], op, qf[nt][2 * (wi + e)]);
+                        op[0] = codes::mul_f16x2(codes::e2m1_f16x2<2>(w0), s0);
+                        op[1] = codes::mul_f16x2(codes::e2m1_f16x2<2>(w1), s1);
+                        op[2] = codes::mul_f16x2(codes::e2m1_f16x2<3>(w0), s0);
+                        op[3] = codes::mul_f16x2(codes::e2m1_f16x2<3>(w1), s1);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], op, qf[nt][2 * (wi + e) + 1]);
+                    }
+                };
+                part(0, __byte_perm(k0, 0, 0x1010), __byte_perm(k1, 0, 0x1010));
+                if constexpr (D == 128) part(2, __byte_perm(k0, 0, 0x3232), __byte_perm(k1, 0, 0x3232));
+            }
+            uint32_t vab = codes::e4m3_f16x2(x.vs & 0xffffu), vcd = codes::e4m3_f16x2(x.vs >> 16);
+            bool grew = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1];
+            if (16 * r + 16 > all_see) {
+                const int tok = 16 * r + 4 * (g / 2) + g % 2;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (tok + (e & 2) >= limit[nt][e & 1]) s[nt][e] = -INFINITY;
+                // what lies past the sequence may be anything
+                const int left = len - 16 * r - 4 * t;
+                if (left < 1) vab &= 0xffff0000u;
+                if (left < 2) vab &= 0x0000ffffu;
+                if (left < 3) vcd &= 0xffff0000u;
+                if (left < 4) vcd &= 0x0000ffffu;
+            }
+            // P is relative to a maximum that may lag the row's: with m five below
+            // the maximum that it was taken from, P is 2^5 there and may grow to
+            // 2^15 before m follows. In f16, so P keeps its 11 bits down to 2^-19 of
+            // the row's largest and is rounded to multiples of 2^-29 of it below.
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) grew |= s[nt][e] > m[nt][e & 1] + 15.f;
+            if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(s[nt][e], s[nt][e + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        top = fmaxf(top - 5.f, m[nt][e]);
+                        const float w = codes::ex2(m[nt][e] - top);
+                        m[nt][e] = top;
+                        l[nt][e] *= w;
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            o[nt][i][e] *= w;
+                            o[nt][i][e + 2] *= w;
+                        }
+                    }
+            }
+            uint32_t p[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = codes::ex2(s[nt][e] - m[nt][e & 1]);
+                l[nt][0] += y[0] + y[2];
+                l[nt][1] += y[1] + y[3];
+                p[nt][0] = transposed(codes::pack_f16(y[0], y[1]));
+                p[nt][1] = transposed(codes::pack_f16(y[2], y[3]));
+            }
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) {
+                // a byte: the same dim of two tokens
+                constexpr uint32_t kLow = 0x0f0f0f0fu;
+                const uint32_t va = x.v[0][w], vb = x.v[1][w], vc = x.v[2][w], vd = x.v[3][w];
+                const uint32_t ab0 = (va & kLow) | ((vb & kLow) << 4), ab1 = ((va >> 4) & kLow) | (vb & ~kLow);
+                const uint32_t cd0 = (vc & kLow) | ((vd & kLow) << 4), cd1 = ((vc >> 4) & kLow) | (vd & ~kLow);
+                uint32_t op[4];
+                operand<0>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w], op, p[nt]);
+                operand<1>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 1], op, p[nt]);
+                operand<2>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 2], op, p[nt]);
+                operand<3>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 3], op, p[nt]);
+            }
+        };
+        for (int r = r0; r < r_end; r += 2 * kWarps) {
+            work(rec[0], r);
+            if (r + 2 * kWarps < r_end) {
+                fetch(rec[0], r + 2 * kWarps, page_next);
+                if (r + 3 * kWarps < r_end) page_next = page_of(r + 3 * kWarps);
+            }
+            if (r + kWarps < r_end) {
+                work(rec[1], r + kWarps);
+                if (r + 3 * kWarps < r_end) {
+                    fetch(rec[1], r + 3 * kWarps, page_next);
+                    if (r + 4 * kWarps < r_end) page_next = page_of(r + 4 * kWarps);
+                }
+            }
+        }
+
+        // ---- the warps' results together
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = l[nt][e];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                const int r = 8 * nt + 2 * t + e;
+                if (g == 0) {
+                    sm[warp][r] = m[nt][e];
+                    sl[warp][r] = x;
+                }
+                float* dst = so + (warp * C::kRows + r) * C::kPitch + g * (D / 8);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[nt][i][e], o[nt][i][e + 2]);
+            }
+        __syncthreads();
+        const bool whole = b0 == 0 && b1 == n_steps;
+        if (threadIdx.x < C::kRows) {
+            const int r = threadIdx.x;
+            float M = kLowest, L = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][r]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float x = codes::ex2(sm[w][r] - M);
+                sw[w][r] = x;
+                L += x * sl[w][r];
+            }
+            sM[r] = M;
+            sL[r] = L;
+            if (whole && r < rows) {
+                const long long at = lse_place(seq, hk, r);
+                const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
+                s_own[r] = j.own;
+                s_other[r] = j.other;
+                if (a.lse) a.lse[at] = j.lse;
+            }
+        }
+        __syncthreads();
+        auto store = [&](int r, int d, float4 x) {  // four dims of a row's result
+            const long long at = place(a.o_st, seq, hk, r) + d;
+            const float own = s_own[r], other = s_other[r];
+            x.x *= own, x.y *= own, x.z *= own, x.w *= own;
+            if (other != 0.f) {
+                const uint2 y = *reinterpret_cast<const uint2*>(a.base_out + at);
+                x.x += other * codes::bf(y.x & 0xffffu), x.y += other * __uint_as_float(y.x & 0xffff0000u);
+                x.z += other * codes::bf(y.y & 0xffffu), x.w += other * __uint_as_float(y.y & 0xffff0000u);
+            }
+            *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(x.x, x.y), ptx::pack_bf16(x.z, x.w));
+        };
+        float* slot = c.partials + (size_t)(2 * blockIdx.x + (b0 > 0 ? 0 : 1)) * C::kSlot;
+        for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(so + (w * C::kRows + r) * C::kPitch + d);
+                const float k = sw[w][r];
+                y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
+            }
+            if (whole)
+                store(r, d, y);
+            else
+                __stcg(reinterpret_cast<float4*>(slot + r * D + d), y);
+        }
+        if (!whole) {
+            if (threadIdx.x < rows)
+                __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * threadIdx.x), make_float2(sM[threadIdx.x], sL[threadIdx.x]));
+            const int first = cta_of(item0), pieces = cta_of(item0 + n_steps - 1) - first + 1;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                __threadfence();
+                s_last = atomicAdd(c.counters + first, 1u) == (unsigned)pieces - 1;
+                if (s_last) {
+                    c.counters[first] = 0;  // for the next launch
+                    __threadfence();
+                }
+            }
+            __syncthreads();
+            if (s_last) {
+                // the piece of CTA first + k: its last share (slot 1) where the item begins in it, else slot 0
+                auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
+                if (threadIdx.x < rows) {
+                    const int r = threadIdx.x;
+                    float M = kLowest, L = 0.f;
+                    for (int k = 0; k < pieces; ++k) M = fmaxf(M, __ldcg(slot_of(k) + C::kRows * D + 2 * r));
+                    for (int k = 0; k < pieces; ++k) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(k) + C::kRows * D + 2 * r));
+                        L += codes::ex2(ml.x - M) * ml.y;
+                    }
+                    sM[r] = M;
+                    const long long at = lse_place(seq, hk, r);
+                    const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
+                    s_own[r] = j.own;
+                    s_other[r] = j.other;
+                    if (a.lse) a.lse[at] = j.lse;
+                }
+                __syncthreads();
+                for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
+                    const int r = x / (D / 4), d = x % (D / 4) * 4;
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int k = 0; k < pieces; ++k) {
+                        const float w = codes::ex2(__ldcg(slot_of(k) + C::kRows * D + 2 * r) - sM[r]);
+                        const float4 z = __ldcg(reinterpret_cast<const float4*>(slot_of(k) + r * D + d));
+                        y.x = fmaf(w, z.x, y.x), y.y = fmaf(w, z.y, y.y), y.z = fmaf(w, z.z, y.z), y.w = fmaf(w, z.w, y.w);
+                    }
+                    store(r, d, y);
+                }
+            }
+        }
+        __syncthreads();  // shared memory is free again
+    }
+}
+
+template <int D, int NT>
+cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+    using C = FewCfg<D, NT>;
+    int sms;
+    cudaError_t e = device_sms(&sms);
+    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
+    if (e != cudaSuccess) return e;
+    const int ctas = sms * (NT == 1 ? 2 : 1);
+    return launch_pdl(cache_few_kernel<D, NT>, dim3(ctas < kCacheMaxCtas ? ctas : kCacheMaxCtas), dim3(32 * kWarps), C::kSmem,
+                      st, c, a, 2);
+}
+
 }  // namespace
 
-cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+cudaError_t launch_cache_attend_simt(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
     const dim3 grid((unsigned)(a.n * a.queries * a.heads));
     return c.D == 128 ? launch_pdl(cache_attend_kernel<128>, grid, dim3(128), 0, st, c, a)
                       : launch_pdl(cache_attend_kernel<64>, grid, dim3(128), 0, st, c, a);
+}
+
+cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+    const long long rows = (long long)a.group * a.queries;
+    if (rows <= 8) return c.D == 128 ? launch_few<128, 1>(c, a, st) : launch_few<64, 1>(c, a, st);
+    if (rows <= 16) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
+    return launch_cache_attend_simt(c, a, st);
 }
 
 }  // namespace msf

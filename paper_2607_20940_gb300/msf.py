@@ -45,7 +45,7 @@ EXPORTS = (
     "msf_unpatchify_tier", "msf_patchify_resample", "msf_mssa_forward_resample",
     "msf_cache_create", "msf_cache_destroy", "msf_cache_query", "msf_cache_bind", "msf_cache_grow",
     "msf_cache_write", "msf_cache_read", "msf_cache_fork", "msf_cache_truncate", "msf_cache_compact",
-    "msf_cache_attend", "msf_cache_device_status",
+    "msf_cache_attend", "msf_cache_attend_simt", "msf_cache_device_status",
 )
 
 
@@ -169,6 +169,7 @@ def _load():
         "msf_cache_truncate": (ctypes.c_int, [P, VP, VP, I32, VP]),
         "msf_cache_compact": (ctypes.c_int, [P, VP]),
         "msf_cache_attend": (ctypes.c_int, [P, I32, VP, I32, ctypes.POINTER(msf_cache_attention), VP]),
+        "msf_cache_attend_simt": (ctypes.c_int, [P, I32, VP, I32, ctypes.POINTER(msf_cache_attention), VP]),
         "msf_cache_device_status": (ctypes.c_int, [P, VP]),
     }
     for name, (res, args) in sig.items():
@@ -486,6 +487,11 @@ def msf_cache_attend(cache: int, layer: int, seqs, n: int, args: msf_cache_atten
     _check(_lib.msf_cache_attend(cache, layer, seqs, n, ctypes.byref(args), _stream(stream)), "msf_cache_attend")
 
 
+def msf_cache_attend_simt(cache: int, layer: int, seqs, n: int, args: msf_cache_attention, stream=None) -> None:
+    _check(_lib.msf_cache_attend_simt(cache, layer, seqs, n, ctypes.byref(args), _stream(stream)),
+           "msf_cache_attend_simt")
+
+
 def msf_cache_device_status(cache: int, stream=None) -> int:
     return _lib.msf_cache_device_status(cache, _stream(stream))
 
@@ -722,9 +728,9 @@ class Cache:
         msf_cache_compact(self.handle, stream)
 
     def attend(self, layer, q, out, lse=None, base_out=None, base_lse=None, seqs=None, causal=False,
-               softmax_scale=0.0, stream=None):
+               softmax_scale=0.0, stream=None, simt=False):
         """Attention of q [rows, queries, heads, head_dim] over the listed sequences, joined with
-        (base_out, base_lse) where given; lse [rows, heads, queries]."""
+        (base_out, base_lse) where given; lse [rows, heads, queries]. simt: on fp32 CUDA cores."""
         import torch
         if q.dim() != 4 or q.shape[3] != self.desc.head_dim:
             raise ValueError(f"q is [rows, queries, heads, {self.desc.head_dim}]")
@@ -742,7 +748,8 @@ class Cache:
                     raise ValueError("base_lse and lse have the same strides")
                 a.lse_strides[:] = strides
         a.queries, a.heads, a.causal, a.softmax_scale = queries, heads, int(causal), softmax_scale
-        msf_cache_attend(self.handle, layer, _list(seqs, n)[0], n, a, stream)
+        call = msf_cache_attend_simt if simt else msf_cache_attend
+        call(self.handle, layer, _list(seqs, n)[0], n, a, stream)
 
     def device_status(self, stream=None) -> int:
         return msf_cache_device_status(self.handle, stream)

@@ -53,7 +53,8 @@ def test_null_and_unbound():
     for call in (("msf_cache_grow", None, None, 1, 1, None), ("msf_cache_write", 0, None, None, 1, 1, 16, 16, s3, None),
                  ("msf_cache_read", 0, None, None, 1, 1, 16, 16, s3, None), ("msf_cache_fork", 4, 4, None, 1, 0, None),
                  ("msf_cache_truncate", None, None, 1, None), ("msf_cache_compact", None),
-                 ("msf_cache_attend", 0, None, 1, ctypes.byref(a), None), ("msf_cache_device_status", None)):
+                 ("msf_cache_attend", 0, None, 1, ctypes.byref(a), None),
+                 ("msf_cache_attend_simt", 0, None, 1, ctypes.byref(a), None), ("msf_cache_device_status", None)):
         assert _status(call[0], None, *call[1:]) == msf.MSF_ERR_INVALID_ARG
         assert _status(call[0], h, *call[1:]) == msf.MSF_ERR_STATE
     msf.msf_cache_destroy(None)

@@ -3,7 +3,9 @@
 Bounds, from the arithmetic: the output's rounding to bf16 is 2^-9 of it; probabilities may
 be rounded to 11 bits on the way, 2^-11 of sum p |v| (A below); a score of D products summed in
 fp32 is off by at most D 2^-24 of scale sum |q k| (B), which changes probabilities by that
-share, twice with the sum. Twice all of it is allowed. The log-sum-exp has the scores' error
+share, twice with the sum. Twice all of it is allowed. Probabilities below 2^-19 of a row's
+largest are multiples of 2^-29 of it (f16's smallest), so each may be 2^-30 off: that counts
+where keys' scores lie far apart (`floor`; the fp32 form has none). The log-sum-exp has the scores' error
 and 2^-20 of one for exponentials and sums."""
 import math
 
@@ -34,7 +36,8 @@ def fill(c, lens, seed, k_std=1.0):
     return oc.quantise(f64(k), c.desc.k_exponent)[0], oc.quantise(f64(v), c.desc.v_exponent)[0]
 
 
-def check(c, kh, vh, lens, q, causal=False, base=None, base_lse=None, scale=None, seqs=None, out=None, lse=None):
+def check(c, kh, vh, lens, q, causal=False, base=None, base_lse=None, scale=None, seqs=None, out=None, lse=None,
+          simt=False, floor=0.0):
     D, r = c.desc.head_dim, q.shape[2] // c.desc.kv_heads
     n, nq = q.shape[:2]
     if out is None:
@@ -43,7 +46,7 @@ def check(c, kh, vh, lens, q, causal=False, base=None, base_lse=None, scale=None
         lse = torch.full((n, q.shape[2], nq), 9.0, device="cuda")
     b = f64(base) if base is not None else None
     bl = f64(base_lse) if base is not None else None
-    c.attend(0, q, out, lse, base, base_lse, ints(seqs), causal, scale or 0.0)
+    c.attend(0, q, out, lse, base, base_lse, ints(seqs), causal, scale or 0.0, simt=simt)
     ok(c)
     got, got_lse, qq = f64(out), f64(lse), f64(q)
     for i in range(n):
@@ -54,6 +57,7 @@ def check(c, kh, vh, lens, q, causal=False, base=None, base_lse=None, scale=None
                                              None if b is None else b[i][:, hs], None if b is None else bl[i, hs])
             share = D * 2.0 ** -24 * B
             bound = 2 * (2.0 ** -9 * np.abs(want) + (2.0 ** -11 + 2 * share) * A) + 1e-30
+            bound += 2 * floor * np.abs(vh[s, :lens[s], h]).sum(0)
             assert (np.abs(got[i][:, hs] - want) <= bound).all(), (i, h, np.max(np.abs(got[i][:, hs] - want) / bound))
             empty = np.isneginf(want_lse)
             assert np.array_equal(empty, np.isneginf(got_lse[i, hs]))
@@ -133,8 +137,9 @@ def test_strides_lists_and_scales():
         assert (hold == 5.0).all() and (lse_hold == 5.0).all()
 
 
+@pytest.mark.parametrize("simt", [True, False])
 @pytest.mark.parametrize("group,queries", [(4, 1), (1, 64)])
-def test_scores_far_apart(group, queries):
+def test_scores_far_apart(group, queries, simt):
     """Rows whose largest score comes late, is huge, or stands alone among keys that do not count."""
     c = make(kv_heads=1, head_dim=128, sequences=3, pages=200, sequence_pages=64)
     lens = [900, 1000, 64]
@@ -142,9 +147,23 @@ def test_scores_far_apart(group, queries):
     q = rows((3, queries, group, 128), 8, 12.0)
     q[1, :, 0] *= 1e-3
     q[0, -1, -1] = 0
-    check(c, kh, vh, lens, q)
-    check(c, kh, vh, lens, q * 2.0 ** -60, scale=2.0 ** 50)
-    check(c, kh, vh, lens, (q * 2.0 ** 40), scale=2.0 ** -41)
+    form = dict(simt=simt, floor=0.0 if simt else 2.0 ** -30)
+    check(c, kh, vh, lens, q, **form)
+    check(c, kh, vh, lens, q * 2.0 ** -60, scale=2.0 ** 50, **form)
+    check(c, kh, vh, lens, (q * 2.0 ** 40), scale=2.0 ** -41, **form)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("group,queries", [(1, 1), (3, 5), (2, 40)])
+def test_fp32_form(group, queries, causal):
+    lens = [0, 1, 17, 300]
+    for D in (64, 128):
+        c = make(kv_heads=2, head_dim=D, sequences=4, sequence_pages=32, pages=60)
+        kh, vh = fill(c, lens, 20)
+        q = rows((4, queries, 2 * group, D), 21)
+        check(c, kh, vh, lens, q, causal, simt=True)
+        base, base_lse = rows(q.shape, 22), torch.ones(4, 2 * group, queries, device="cuda")
+        check(c, kh, vh, lens, q, causal, base, base_lse, simt=True)
 
 
 @pytest.mark.parametrize("group,queries", [(8, 1), (1, 1), (1, 200), (2, 33)])
