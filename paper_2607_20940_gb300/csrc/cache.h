@@ -98,6 +98,7 @@ struct CacheRows {
 cudaError_t launch_cache_write(const CacheView& c, const CacheRows& r, const uint16_t* k, const uint16_t* v, cudaStream_t st);
 cudaError_t launch_cache_read(const CacheView& c, const CacheRows& r, uint16_t* k, uint16_t* v, cudaStream_t st);
 cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st);
+cudaError_t launch_cache_attend_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st);
 cudaError_t launch_cache_attend_simt(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st);
 
 }  // namespace msf

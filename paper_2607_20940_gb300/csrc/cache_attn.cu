@@ -381,8 +381,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
                 }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                f[nt][x] = codes::row_down(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x))) * (a.scale * c.k_unit) *
-                           1.4426950408889634f;
+                f[nt][x] = codes::row_factor(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x)), a.scale * c.k_unit);
                 const int rr = 8 * nt + 2 * t + x;
                 limit[nt][x] = rr >= rows ? 0 : a.causal ? len - a.queries + 1 + rr / a.group : len;
             }
@@ -667,7 +666,7 @@ cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cuda
     const long long rows = (long long)a.group * a.queries;
     if (rows <= 8) return c.D == 128 ? launch_few<128, 1>(c, a, st) : launch_few<64, 1>(c, a, st);
     if (rows <= 16) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
-    return launch_cache_attend_simt(c, a, st);
+    return launch_cache_attend_many(c, a, st);
 }
 
 }  // namespace msf

@@ -56,6 +56,11 @@ __device__ __forceinline__ float bf(uint32_t x16) { return __uint_as_float(x16 <
 __device__ __forceinline__ int row_exponent(uint32_t largest_bf16) { return max((int)(largest_bf16 >> 7), 28); }
 __device__ __forceinline__ float row_up(int e) { return __uint_as_float((uint32_t)(268 - e) << 23); }
 __device__ __forceinline__ float row_down(int e) { return __uint_as_float((uint32_t)(e - 14) << 23); }
+// What takes a score of such a row to base 2; never 0 or infinite, so that a
+// masked score stays -infinity and a row of zeros 0.
+__device__ __forceinline__ float row_factor(int e, float scale) {
+    return fminf(fmaxf(row_down(e) * scale * 1.4426950408889634f, 1.17549435e-38f), 3.0e38f);
+}
 
 // The joined result's weights: this attention's unnormalised output times own,
 // the base's times other. M: running maximum (base 2), L: sum.

@@ -1,0 +1,713 @@
+// Attention of many queries over the 4-bit cache on the sm_103a tensor cores.
+//
+// Work: an item is a block of up to 256 rows (two tiles of 128) of one sequence
+// and key head; a row is a query of one of the heads that share the key head,
+// the heads of a query next to each other. An item walks its sequence (causal:
+// as far as its last row sees) in steps of 128 tokens. All items' steps, weighted
+// by their tiles, form one sequence that the CTAs (one per SM) share evenly. A
+// piece that is not a whole item leaves its unnormalised output, maximum and sum
+// in a slot; the last CTA of an item to finish adds its pieces in order.
+//
+// Roles (512 threads):
+//   warp 0      MMA issuer: S_t = Q_t K^T (both from shared memory), O_t += P_t V
+//               (P from TMEM), f16 in fp32
+//   warp 1      TMEM (all 512 columns)
+//   warps 4-7   codes to f16: a step's codes and scales of K and then of V from
+//               global memory into registers, one step ahead; code times scale,
+//               which f16 holds exactly, into 128-byte-swizzled tiles
+//   warps 8-11  softmax of tile 0, warps 12-15 of tile 1: a thread per row. They
+//               also put Q into shared memory, as f16 with the row's largest value
+//               near 2^14 (the row's power of two joins the softmax scale)
+// TMEM columns: S0 [0,128) S1 [128,256) O0 [256,256+D) O1 [384,384+D).
+// P is written as f16 over S. The issuer puts S_t of the next step right after
+// O_t of this one, so the commit that says S_t is ready covers both, and a softmax
+// warp that sees it may rescale O_t in place.
+//
+// Bound: the tensor pipe (4 D operations per row and token) with many rows, HBM
+// (9/8 D bytes a token) with few. Every wait is bounded.
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "cache.h"
+#include "cache_codes.cuh"
+#include "internal.h"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace msf {
+namespace {
+
+constexpr int kTile = 128;  // rows of a tile, tokens of a step
+constexpr int kBlock = 2 * kTile;
+constexpr int kThreads = 512;
+constexpr int kK = 2, kV = 3;  // tiles of K and V in shared memory
+constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
+constexpr float kLowest = -3.402823466e38f;
+// 128 registers a thread at launch, shared out anew.
+constexpr int kLaunchRegs = 128, kCtrlRegs = 56, kCodeRegs = 88, kSoftmaxRegs = 184;
+static_assert(4 * kCtrlRegs + 4 * kCodeRegs + 8 * kSoftmaxRegs <= 16 * kLaunchRegs, "register split");
+
+template <int D>
+struct ManyCfg {
+    static constexpr int kBytes = kTile * D * 2;  // of a tile in shared memory
+    static constexpr int kUsed = (2 + kK + kV) * kBytes + 1024;
+    static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;  // one CTA per SM (all of TMEM)
+    static constexpr size_t kSlot = (size_t)kBlock * (D + 2);  // floats of a partial result
+};
+static_assert(ManyCfg<128>::kSmem + 1024 <= 227 * 1024, "shared memory of the launch");
+static_assert(2 * 160 * ManyCfg<128>::kSlot <= kCachePartialFloats, "partial results");
+
+// The items of a call and a CTA's pieces of them, in order. Every thread walks by itself.
+struct Piece {
+    int seq, hk, blk;  // row of the list, key head, block
+    int len;           // of the sequence
+    int rows, tiles;   // of the block
+    int steps, b0, b1; // of the item; this piece's
+    long long item0;   // the item's first unit (a step of one tile)
+};
+
+struct Walk {
+    const CacheView& c;
+    const CacheAttnArgs& a;
+    int rows, blocks;
+    long long u0, u1;  // this CTA's units
+    int seq, hk, blk, len;
+    long long at;  // first unit of the next item
+
+    __device__ Walk(const CacheView& c_, const CacheAttnArgs& a_)
+        : c(c_), a(a_), rows(a_.group * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
+    __device__ int length(int i) const {
+        const int s = a.seqs ? a.seqs[i] : i;
+        return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
+    }
+    __device__ int block_rows(int b) const { return min(kBlock, rows - b * kBlock); }
+    __device__ int tiles(int b) const { return (block_rows(b) + kTile - 1) / kTile; }
+    __device__ int steps(int n, int b) const {
+        if (a.causal) n = min(n, max(0, n - a.queries + 1 + (b * kBlock + block_rows(b) - 1) / a.group));
+        return (n + kTile - 1) / kTile;
+    }
+    __device__ long long head_units(int n) const {
+        if (!a.causal) return (long long)((n + kTile - 1) / kTile) * ((rows + kTile - 1) / kTile);
+        long long u = 0;
+        for (int b = 0; b < blocks; ++b) u += (long long)steps(n, b) * tiles(b);
+        return u;
+    }
+    // Begin in sequence `i`, whose first unit is `first`.
+    __device__ void begin(int i, long long first, long long u0_, long long u1_) {
+        u0 = u0_, u1 = u1_;
+        seq = i;
+        len = length(i);
+        const long long per = head_units(len);
+        hk = (int)((u0 - first) / per);
+        at = first + hk * per;
+        blk = 0;
+    }
+    __device__ bool next(Piece& p) {
+        while (at < u1) {
+            const int n = steps(len, blk), w = tiles(blk);
+            const long long first = at;
+            p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
+            p.rows = block_rows(blk), p.tiles = w, p.steps = n, p.item0 = first;
+            at += (long long)n * w;
+            // step k belongs to the CTA that has unit first + k w
+            p.b0 = (int)min((long long)n, max(0ll, (u0 - first + w - 1) / w));
+            if (u0 <= first) p.b0 = 0;
+            p.b1 = (int)min((long long)n, (u1 - first + w - 1) / w);
+            if (++blk == blocks) {
+                blk = 0;
+                if (++hk == c.Hk) {
+                    hk = 0;
+                    if (at < u1) {
+                        do len = length(++seq);
+                        while (len == 0);
+                    }
+                }
+            }
+            if (p.b0 < p.b1) return true;
+        }
+        return false;
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView c, const CacheAttnArgs a, long long wait_limit) {
+    using C = ManyCfg<D>;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    unsigned char* sQ = smem;
+    unsigned char* sK = smem + 2 * C::kBytes;
+    unsigned char* sV = sK + kK * C::kBytes;
+    __shared__ uint64_t q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
+    __shared__ uint64_t s_full[2], p_full[2], o_full, drained;
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_flag, s_last;
+    __shared__ long long s_scan[kThreads / 32], s_found[2];
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        ptx::mbar_init(&q_full, 8);
+        for (int s = 0; s < kK; ++s) {
+            ptx::mbar_init(&k_full[s], 4);
+            ptx::mbar_init(&k_empty[s], 1);
+        }
+        for (int s = 0; s < kV; ++s) {
+            ptx::mbar_init(&v_full[s], 4);
+            ptx::mbar_init(&v_empty[s], 1);
+        }
+        for (int t = 0; t < 2; ++t) {
+            ptx::mbar_init(&s_full[t], 1);
+            ptx::mbar_init(&p_full[t], 4);
+        }
+        ptx::mbar_init(&o_full, 1);
+        ptx::mbar_init(&drained, 1);
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(&tmem_base_sh, 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tbase = tmem_base_sh;
+    volatile int* abort_p = &abort_flag;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+
+    Walk walk(c, a);
+    auto place = [&](const long long* st, int i, int hk, int r) {
+        return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
+    };
+    auto lse_place = [&](int i, int hk, int r) {
+        return i * a.l_st[0] + (hk * a.group + r % a.group) * a.l_st[1] + r / a.group;
+    };
+
+    // ---- blocks that see no token: their rows are empty, or the base's
+    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * walk.blocks; x += gridDim.x) {
+        const int b = (int)(x % walk.blocks), hk = (int)(x / walk.blocks % c.Hk), i = (int)(x / walk.blocks / c.Hk);
+        if (walk.steps(walk.length(i), b) > 0) continue;
+        if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
+        const int n = walk.block_rows(b);
+        for (int y = threadIdx.x; y < n * (D / 8); y += kThreads) {
+            const int r = b * kBlock + y / (D / 8), d = y % (D / 8) * 8;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
+                w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
+            *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+        }
+        if (a.lse && a.lse != a.base_lse)
+            for (int y = threadIdx.x; y < n; y += kThreads) {
+                const long long at = lse_place(i, hk, b * kBlock + y);
+                a.lse[at] = a.base_lse ? a.base_lse[at] : -INFINITY;
+            }
+    }
+
+    // ---- this CTA's share
+    auto scan = [&](long long x, long long& all) {
+        long long v = x;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const long long y = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += y;
+        }
+        if (lane == 31) s_scan[warp] = v;
+        __syncthreads();
+        long long before = 0;
+        all = 0;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += s_scan[w];
+            all += s_scan[w];
+        }
+        __syncthreads();
+        return before + v - x;
+    };
+    long long U = 0, mine = 0;
+    for (int i = threadIdx.x; i < a.n; i += kThreads) mine += walk.head_units(walk.length(i));
+    scan(mine, U);
+    U *= c.Hk;
+    const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
+    const bool idle = (int)blockIdx.x >= G || U == 0;
+    const long long u0 = idle ? 0 : U * blockIdx.x / G, u1 = idle ? 0 : U * (blockIdx.x + 1) / G;
+    auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
+    if (!idle) {
+        long long base = 0;
+        for (int i0 = 0; i0 < a.n; i0 += kThreads) {
+            const int i = i0 + (int)threadIdx.x;
+            const long long x = i < a.n ? walk.head_units(walk.length(i)) * c.Hk : 0;
+            long long all;
+            const long long before = base + scan(x, all);
+            if (u0 >= before && u0 < before + x) {
+                s_found[0] = i;
+                s_found[1] = before;
+            }
+            base += all;
+            if (u0 < base) break;
+        }
+        __syncthreads();
+        walk.begin((int)s_found[0], s_found[1], u0, u1);
+    } else {
+        walk.at = walk.u1 = 0;  // no pieces
+    }
+
+    bool ok = true;
+    Piece pc;
+    if (warp < 4) {
+        ptx::setmaxnreg_dec<kCtrlRegs>();
+        if (warp == 0) {
+            // ============================= MMA issuer =============================
+            constexpr uint32_t idS = ptx::idesc_f16(kTile, kTile, false, false);
+            constexpr uint32_t idO = ptx::idesc_f16(kTile, D, false, true);
+            constexpr uint64_t kTileDesc = (uint64_t)(C::kBytes >> 4);
+            const uint64_t q_desc = ptx::sdesc_sw128(ptx::smem_u32(sQ), 16, 1024);
+            const uint64_t k_desc = ptx::sdesc_sw128(ptx::smem_u32(sK), 16, 1024);
+            const uint64_t v_desc = ptx::sdesc_sw128(ptx::smem_u32(sV), kTile * 128, 1024);
+            int nk = 0, nv = 0, pieces = 0, np[2] = {0, 0};
+            auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+                const bool r = ptx::mbar_wait_bounded(bar, parity, abort_p, wait_limit);
+                return __all_sync(0xffffffffu, r);
+            };
+            auto scores = [&](int t) {  // S_t = Q_t K^T, K the tile nk
+                const uint64_t kd = k_desc + (uint64_t)(nk % kK) * kTileDesc, qd = q_desc + (uint64_t)t * kTileDesc;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint64_t off = (uint64_t)(((kk / 4) * (kTile * 128) + (kk % 4) * 32) >> 4);
+                    ptx::mma_ss(tbase + t * 128, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
+                }
+            };
+            while (ok && walk.next(pc)) {
+                const int n = pc.b1 - pc.b0, T = pc.tiles;
+                ok = wait_all(&q_full, (uint32_t)(pieces & 1)) && wait_all(&k_full[nk % kK], (uint32_t)((nk / kK) & 1));
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (ptx::elect_one_sync()) {
+                    for (int t = 0; t < T; ++t) {
+                        scores(t);
+                        ptx::mma_commit(&s_full[t]);
+                    }
+                    ptx::mma_commit(&k_empty[nk % kK]);
+                }
+                __syncwarp();
+                ++nk;
+                for (int j = 0; j < n && ok; ++j) {
+                    const bool more = j + 1 < n;
+                    const int vs = nv % kV;
+                    ok = wait_all(&v_full[vs], (uint32_t)((nv / kV) & 1)) &&
+                         (!more || wait_all(&k_full[nk % kK], (uint32_t)((nk / kK) & 1)));
+                    for (int t = 0; t < T && ok; ++t) {
+                        ok = wait_all(&p_full[t], (uint32_t)(np[t] & 1));
+                        if (!ok) break;
+                        ++np[t];
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one_sync()) {
+                            const uint64_t vd = v_desc + (uint64_t)vs * kTileDesc;
+#pragma unroll
+                            for (int kk = 0; kk < kTile / 16; ++kk)
+                                ptx::mma_ts(tbase + 256 + t * 128, tbase + t * 128 + kk * 8, vd + (uint64_t)(kk * (2048 >> 4)),
+                                            idO, (j > 0 || kk > 0) ? 1u : 0u);
+                            if (more) {
+                                scores(t);
+                                ptx::mma_commit(&s_full[t]);
+                            }
+                            if (t == T - 1) {
+                                ptx::mma_commit(&v_empty[vs]);
+                                if (more) ptx::mma_commit(&k_empty[nk % kK]);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    ++nv;
+                    if (more) ++nk;
+                }
+                if (!ok) break;
+                if (ptx::elect_one_sync()) ptx::mma_commit(&o_full);
+                __syncwarp();
+                ++pieces;
+            }
+            if (!ok) {
+                // every product issued is done before its operands' space goes
+                if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
+                if (ptx::elect_one_sync()) ptx::mma_commit(&drained);
+                __syncwarp();
+                volatile int never = 0;
+                ptx::mbar_wait_bounded(&drained, 0, &never, kWaitLimit);
+            }
+        }
+    } else if (warp < 8) {
+        ptx::setmaxnreg_dec<kCodeRegs>();
+        // ============================ codes to f16 ============================
+        // A unit is 32 neighbouring dims of a token: 16 bytes of codes, two
+        // scales, 64 bytes of f16. Thread x of iteration i has unit 128 i + x of
+        // the step: lanes read whole rows.
+        constexpr int kIt = D / 32, kPer = 16 * (D / 32);  // iterations; units of a record
+        const int x = (int)threadIdx.x - 128;
+        const int chunk = x % (D / 32), tok = x % kPer / (D / 32), rec0 = x / kPer;
+        constexpr int kRecStep = 128 / kPer;  // records per iteration
+        uint4 kc[kIt], vc[kIt];
+        uint32_t ks[kIt], vs[kIt];  // f16 pairs of the two scales
+        int page[kIt];
+        // 16-byte slots of the unit's row: the order in which a lane writes them
+        // keeps eight lanes' stores in eight different slots
+        const int turn = D == 128 ? 2 * (chunk >> 1) : 0;
+        const uint32_t row_base = (uint32_t)((chunk >> 1) * (kTile * 128)), slot0 = (uint32_t)((chunk & 1) * 4);
+        Piece nx;
+        int j = 0;
+        bool have = walk.next(nx);
+        if (have) j = nx.b0;
+        auto record_of = [&](int i) { return 8 * j + rec0 + kRecStep * i; };
+        auto pages = [&]() {
+            const int* row = c.table + (size_t)(a.seqs ? a.seqs[nx.seq] : nx.seq) * c.W;
+#pragma unroll
+            for (int i = 0; i < kIt; ++i) {
+                const int r = record_of(i);
+                page[i] = 16 * r < nx.len ? row[r >> (c.log2_p - 4)] : -1;
+            }
+        };
+        auto base_of = [&](int i) {
+            return c.pool + ((long long)a.layer * c.pages + page[i]) * c.page_bytes +
+                   (long long)(nx.hk * (c.P / 16) + (record_of(i) & (c.P / 16 - 1))) * cache_record_bytes(D);
+        };
+        auto load_k = [&]() {
+#pragma unroll
+            for (int i = 0; i < kIt; ++i) {
+                kc[i] = make_uint4(0u, 0u, 0u, 0u);
+                ks[i] = 0;
+                if (cache_page_ok(c, page[i])) {
+                    const uint8_t* p = base_of(i);
+                    kc[i] = *reinterpret_cast<const uint4*>(p + tok * (D / 2) + chunk * 16);
+                    ks[i] = *reinterpret_cast<const uint16_t*>(p + cache_k_scales(D) + tok * (D / 16) + chunk * 2);
+                }
+            }
+        };
+        auto load_v = [&]() {
+#pragma unroll
+            for (int i = 0; i < kIt; ++i) {
+                vc[i] = make_uint4(0u, 0u, 0u, 0u);
+                vs[i] = 0;
+                // tokens past the sequence: zeros
+                if (cache_page_ok(c, page[i]) && 16 * record_of(i) + tok < nx.len) {
+                    const uint8_t* p = base_of(i);
+                    vc[i] = *reinterpret_cast<const uint4*>(p + cache_v_codes(D) + tok * (D / 2) + chunk * 16);
+                    const uint8_t* q = p + cache_v_scales(D) + chunk * 32 + tok;
+                    vs[i] = q[0] | (uint32_t)q[16] << 8;
+                }
+            }
+        };
+        auto put = [&](unsigned char* tile, const uint4 (&w)[kIt], const uint32_t (&sc)[kIt]) {
+#pragma unroll
+            for (int i = 0; i < kIt; ++i) {
+                const int r = 16 * (rec0 + kRecStep * i) + tok;  // row of the tile
+                const uint32_t two = codes::e4m3_f16x2(sc[i]);
+                const uint32_t s0 = __byte_perm(two, 0, 0x1010), s1 = __byte_perm(two, 0, 0x3232);
+                const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                unsigned char* row = tile + row_base + r * 128;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    // the slot's number within the unit depends on the lane, so the word is selected, not indexed
+                    const uint32_t y = turn ? cw[q ^ 2] : cw[q], s = (q ^ turn) < 2 ? s0 : s1;
+                    uint4 o;
+                    o.x = codes::mul_f16x2(codes::e2m1_f16x2<0>(y), s);
+                    o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(y), s);
+                    o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(y), s);
+                    o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(y), s);
+                    *reinterpret_cast<uint4*>(row + (((slot0 + (q ^ turn)) ^ (r & 7)) << 4)) = o;
+                }
+            }
+        };
+        int nk = 0, nv = 0;
+        auto give = [&](uint64_t* bar) {
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar);
+        };
+        if (have) {
+            pages();
+            load_k();
+            load_v();
+        }
+        while (have) {
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&k_empty[nk % kK], (uint32_t)((nk / kK) & 1) ^ 1u, abort_p, wait_limit));
+            if (!ok) break;
+            put(sK + (nk % kK) * C::kBytes, kc, ks);
+            give(&k_full[nk % kK]);
+            ++nk;
+            if (++j == nx.b1) {
+                have = walk.next(nx);
+                if (have) j = nx.b0;
+            }
+            if (have) {
+                pages();
+                load_k();
+            }
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&v_empty[nv % kV], (uint32_t)((nv / kV) & 1) ^ 1u, abort_p, wait_limit));
+            if (!ok) break;
+            put(sV + (nv % kV) * C::kBytes, vc, vs);
+            give(&v_full[nv % kV]);
+            ++nv;
+            if (have) load_v();
+        }
+        if (!ok && lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
+    } else {
+        ptx::setmaxnreg_inc<kSoftmaxRegs>();
+        // =================== softmax: one thread per row ===================
+        const int t = (warp - 8) / 4, wq = warp % 4;
+        const int r = wq * 32 + lane;  // row of the tile
+        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        const uint32_t tS = tbase + t * 128 + lane_off, tO = tbase + 256 + t * 128 + lane_off;
+        int ns = 0, pieces = 0;
+        while (ok && walk.next(pc)) {
+            const int R = pc.blk * kBlock + t * kTile + r;  // row of (sequence, key head)
+            const bool live = t * kTile + r < pc.rows;
+            float f = 0.f;      // to base-2 scores
+            int limit = 0;      // tokens that the row sees
+            if (t < pc.tiles) {
+                // ---- Q
+                uint32_t w[D / 2];
+                if (live) {
+                    const uint16_t* q = a.q + place(a.q_st, pc.seq, pc.hk, R);
+#pragma unroll
+                    for (int e = 0; e < D / 8; ++e) {
+                        const uint4 y = *reinterpret_cast<const uint4*>(q + 8 * e);
+                        w[4 * e] = y.x, w[4 * e + 1] = y.y, w[4 * e + 2] = y.z, w[4 * e + 3] = y.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < D / 2; ++e) w[e] = 0u;
+                }
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < D / 2; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+                const int e2 = codes::row_exponent(top);
+                const float up = codes::row_up(e2);
+                f = codes::row_factor(e2, a.scale * c.k_unit);
+                limit = !live ? 0 : a.causal ? pc.len - a.queries + 1 + R / a.group : pc.len;
+#pragma unroll
+                for (int e = 0; e < D / 8; ++e) {
+                    uint32_t y[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        y[z] = codes::pack_f16(codes::bf(w[4 * e + z] & 0xffffu) * up, __uint_as_float(w[4 * e + z] & 0xffff0000u) * up);
+                    *reinterpret_cast<uint4*>(sQ + t * C::kBytes + (e / 8) * (kTile * 128) + r * 128 + (((e % 8) ^ (r & 7)) << 4)) =
+                        make_uint4(y[0], y[1], y[2], y[3]);
+                }
+                ptx::fence_proxy_async_smem();
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&q_full);
+
+            float m = kLowest, l = 0.f;
+            if (t < pc.tiles) {
+                for (int j = pc.b0; j < pc.b1; ++j, ++ns) {
+                    ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&s_full[t], (uint32_t)(ns & 1), abort_p, wait_limit));
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) ptx::tmem_ld32(tS + 32 * q4, s[q4]);
+                    ptx::tmem_wait_ld();
+                    const int valid = limit - j * kTile;
+                    if (valid < kTile) {
+#pragma unroll
+                        for (int e = 0; e < 128; ++e)
+                            if (e >= valid) s[e >> 5][e & 31] = 0xff800000u;
+                    }
+                    auto tile_max = [&]() -> float {  // five below: P is 2^5 at the maximum
+                        float mx[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mx[e] = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 128; e += 2)
+                            mx[(e >> 1) & 7] = ptx::fmax3(mx[(e >> 1) & 7], __uint_as_float(s[e >> 5][e & 31]),
+                                                          __uint_as_float(s[e >> 5][(e & 31) + 1]));
+                        return fmaxf(ptx::fmax3(mx[0], mx[1], mx[2]),
+                                     fmaxf(ptx::fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * f - 5.f;
+                    };
+                    if (j == pc.b0) m = fmaxf(tile_max(), kLowest);
+                    uint64_t sum2[2];
+                    // The maximum may lag the row's until a tile's sum passes 2^15,
+                    // which f16 holds.
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        const float nm = -m;
+                        const uint64_t fx2 = ptx::f2_pack(f, f), nmx2 = ptx::f2_pack(nm, nm);
+                        sum2[0] = sum2[1] = ptx::f2_pack(0.f, 0.f);
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const uint64_t arg = ptx::f2_fma(
+                                    ptx::f2_pack(__uint_as_float(s[q4][2 * e]), __uint_as_float(s[q4][2 * e + 1])), fx2, nmx2);
+                                float a0, a1;
+                                ptx::f2_unpack(arg, a0, a1);
+                                const float p0 = codes::ex2(a0), p1 = codes::ex2(a1);
+                                sum2[e & 1] = ptx::f2_add(sum2[e & 1], ptx::f2_pack(p0, p1));
+                                pk[e] = codes::pack_f16(p0, p1);
+                            }
+                            ptx::tmem_st16(tS + 16 * q4, pk);
+                        }
+                        if (pass == 1) break;
+                        float a0, a1, b0, b1;
+                        ptx::f2_unpack(sum2[0], a0, a1);
+                        ptx::f2_unpack(sum2[1], b0, b1);
+                        const float tile_sum = (a0 + a1) + (b0 + b1);
+                        if (!__any_sync(0xffffffffu, !(tile_sum <= 32768.0f))) break;
+                        const float m_new = fmaxf(m, tile_max());
+                        const float k = codes::ex2(m - m_new);
+                        l *= k;
+                        m = m_new;
+                        if (j > pc.b0) {
+#pragma unroll 1
+                            for (int e = 0; e < D / 16; ++e) {
+                                uint32_t o[16];
+                                ptx::tmem_ld16(tO + e * 16, o);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * k);
+                                ptx::tmem_st16(tO + e * 16, o);
+                            }
+                        }
+                        ptx::tmem_wait_st();  // P of the first pass is overwritten after this
+                    }
+                    {
+                        float a0, a1, b0, b1;
+                        ptx::f2_unpack(sum2[0], a0, a1);
+                        ptx::f2_unpack(sum2[1], b0, b1);
+                        l += (a0 + a1) + (b0 + b1);
+                    }
+                    ptx::tmem_wait_st();
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&p_full[t]);
+                }
+            }
+            ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
+            ok = ptx::named_bar_and(1, 256, ok);
+            ++pieces;
+            if (!ok) break;
+            ptx::tc_fence_after();
+
+            // ---- the piece's result
+            const bool whole = pc.b0 == 0 && pc.b1 == pc.steps;
+            codes::Join jn;
+            const long long out_at = live ? place(a.o_st, pc.seq, pc.hk, R) : 0;
+            auto finish = [&](float M, float L) {
+                const long long at = lse_place(pc.seq, pc.hk, R);
+                jn = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
+                if (a.lse) a.lse[at] = jn.lse;
+            };
+            auto store = [&](int d, const uint32_t (&o)[32]) {  // 32 dims of the row's result
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y[8];
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[8 * e + z]) * jn.own;
+                    const long long at = out_at + d + 8 * e;
+                    if (jn.other != 0.f) {
+                        const uint4 b = *reinterpret_cast<const uint4*>(a.base_out + at);
+                        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            y[2 * z] += jn.other * codes::bf(bw[z] & 0xffffu);
+                            y[2 * z + 1] += jn.other * __uint_as_float(bw[z] & 0xffff0000u);
+                        }
+                    }
+                    *reinterpret_cast<uint4*>(a.out + at) = make_uint4(ptx::pack_bf16(y[0], y[1]), ptx::pack_bf16(y[2], y[3]),
+                                                                       ptx::pack_bf16(y[4], y[5]), ptx::pack_bf16(y[6], y[7]));
+                }
+            };
+            // A slot: [D / 4][256 rows] of four dims, then [256 rows] of maximum and sum: a warp's accesses are whole lines.
+            float* slot = c.partials + (size_t)(2 * blockIdx.x + (pc.b0 > 0 ? 0 : 1)) * C::kSlot;
+            const int sr = t * kTile + r;
+            if (t < pc.tiles) {
+                if (whole && live) finish(m, l);
+#pragma unroll 1
+                for (int d = 0; d < D; d += 32) {
+                    uint32_t o[32];
+                    ptx::tmem_ld32(tO + d, o);
+                    ptx::tmem_wait_ld();
+                    if (whole) {
+                        if (live) store(d, o);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            __stcg(reinterpret_cast<float4*>(slot) + (d / 4 + e) * kBlock + sr,
+                                   make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                               __uint_as_float(o[4 * e + 3])));
+                    }
+                }
+                if (!whole) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
+            }
+            ptx::tc_fence_before();
+            if (!whole) {
+                const int first = cta_of(pc.item0), n = cta_of(pc.item0 + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
+                ptx::named_bar_sync(1, 256);
+                if (threadIdx.x == 256) {
+                    __threadfence();
+                    s_last = atomicAdd(c.counters + first, 1u) == (unsigned)n - 1;
+                    if (s_last) {
+                        c.counters[first] = 0;  // for the next launch
+                        __threadfence();
+                    }
+                }
+                ptx::named_bar_sync(1, 256);
+                if (s_last && live) {
+                    auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
+                    float M = kLowest, L = 0.f;
+                    for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr).x);
+                    for (int k = 0; k < n; ++k) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr);
+                        L += codes::ex2(ml.x - M) * ml.y;
+                    }
+                    finish(M, L);
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 32) {
+                        uint32_t o[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+#pragma unroll 1
+                        for (int k = 0; k < n; ++k) {
+                            const float w = codes::ex2(__ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr).x - M);
+                            float4 y[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(slot_of(k)) + (d / 4 + e) * kBlock + sr);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                o[4 * e] = __float_as_uint(fmaf(w, y[e].x, __uint_as_float(o[4 * e])));
+                                o[4 * e + 1] = __float_as_uint(fmaf(w, y[e].y, __uint_as_float(o[4 * e + 1])));
+                                o[4 * e + 2] = __float_as_uint(fmaf(w, y[e].z, __uint_as_float(o[4 * e + 2])));
+                                o[4 * e + 3] = __float_as_uint(fmaf(w, y[e].w, __uint_as_float(o[4 * e + 3])));
+                            }
+                        }
+                        store(d, o);
+                    }
+                }
+            }
+        }
+        if (!ok && lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
+    }
+    __syncwarp();
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tbase, 512);
+    }
+}
+
+template <int D>
+cudaError_t launch_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+    int sms;
+    cudaError_t e = device_sms(&sms);
+    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_many_kernel<D>, ManyCfg<D>::kSmem, -1, kLaunchRegs);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(cache_many_kernel<D>, dim3(sms < 160 ? sms : 160), dim3(kThreads), ManyCfg<D>::kSmem, st, c, a, kWaitLimit);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_attend_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+    return c.D == 128 ? launch_many<128>(c, a, st) : launch_many<64>(c, a, st);
+}
+
+}  // namespace msf
