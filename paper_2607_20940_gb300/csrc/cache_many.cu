@@ -12,6 +12,7 @@
 //   warp 0      MMA issuer: S_t = Q_t K^T (both from shared memory), O_t += P_t V
 //               (P from TMEM), f16 in fp32
 //   warp 1      TMEM (all 512 columns)
+//   warp 2      the CTA's pieces, into a ring that the others read
 //   warps 4-7   codes to f16: a step's codes and scales of K and then of V from
 //               global memory into registers, one step ahead; code times scale,
 //               which f16 holds exactly, into 128-byte-swizzled tiles
@@ -57,14 +58,16 @@ struct ManyCfg {
 static_assert(ManyCfg<128>::kSmem + 1024 <= 227 * 1024, "shared memory of the launch");
 static_assert(2 * 160 * ManyCfg<128>::kSlot <= kCachePartialFloats, "partial results");
 
-// The items of a call and a CTA's pieces of them, in order. Every thread walks by itself.
+// A CTA's pieces of the call's items, in order. One warp finds them and hands them
+// to the others through a ring in shared memory.
 struct Piece {
-    int seq, hk, blk;  // row of the list, key head, block
-    int len;           // of the sequence
-    int rows, tiles;   // of the block
-    int steps, b0, b1; // of the item; this piece's
-    long long item0;   // the item's first unit (a step of one tile)
+    int seq, hk, blk;   // row of the list, key head, block
+    int len;            // of the sequence
+    int rows, tiles;    // of the block
+    int steps, b0, b1;  // of the item; this piece's. steps 0: no more
+    int first, pieces;  // the CTAs that have the item
 };
+constexpr int kPieces = 4;
 
 struct Walk {
     const CacheView& c;
@@ -102,17 +105,23 @@ struct Walk {
         at = first + hk * per;
         blk = 0;
     }
-    __device__ bool next(Piece& p) {
+    __device__ bool next(Piece& p, int G, long long U) {
+        auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
         while (at < u1) {
             const int n = steps(len, blk), w = tiles(blk);
             const long long first = at;
             p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
-            p.rows = block_rows(blk), p.tiles = w, p.steps = n, p.item0 = first;
+            p.rows = block_rows(blk), p.tiles = w, p.steps = n;
             at += (long long)n * w;
             // step k belongs to the CTA that has unit first + k w
             p.b0 = (int)min((long long)n, max(0ll, (u0 - first + w - 1) / w));
             if (u0 <= first) p.b0 = 0;
             p.b1 = (int)min((long long)n, (u1 - first + w - 1) / w);
+            const bool take = p.b0 < p.b1;
+            if (take) {
+                p.first = cta_of(first);
+                p.pieces = cta_of(first + (long long)(n - 1) * w) - p.first + 1;
+            }
             if (++blk == blocks) {
                 blk = 0;
                 if (++hk == c.Hk) {
@@ -123,7 +132,7 @@ struct Walk {
                     }
                 }
             }
-            if (p.b0 < p.b1) return true;
+            if (take) return true;
         }
         return false;
     }
@@ -139,6 +148,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     unsigned char* sV = sK + kK * C::kBytes;
     __shared__ uint64_t q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
     __shared__ uint64_t s_full[2], p_full[2], o_full, drained;
+    __shared__ uint64_t pc_full[kPieces], pc_empty[kPieces];
+    __shared__ Piece ring[kPieces];
     __shared__ uint32_t tmem_base_sh;
     __shared__ int abort_flag, s_last;
     __shared__ long long s_scan[kThreads / 32], s_found[2];
@@ -158,6 +169,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&s_full[t], 1);
             ptx::mbar_init(&p_full[t], 4);
+        }
+        for (int s = 0; s < kPieces; ++s) {
+            ptx::mbar_init(&pc_full[s], 1);
+            ptx::mbar_init(&pc_empty[s], 13);  // warps that read pieces
         }
         ptx::mbar_init(&o_full, 1);
         ptx::mbar_init(&drained, 1);
@@ -229,7 +244,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
     const bool idle = (int)blockIdx.x >= G || U == 0;
     const long long u0 = idle ? 0 : U * blockIdx.x / G, u1 = idle ? 0 : U * (blockIdx.x + 1) / G;
-    auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
     if (!idle) {
         long long base = 0;
         for (int i0 = 0; i0 < a.n; i0 += kThreads) {
@@ -251,10 +265,36 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     }
 
     bool ok = true;
+    // The readers' side of the ring: the n-th piece, and that a warp is done with it.
+    auto piece = [&](int n, Piece& p) {
+        ok = ok && ptx::mbar_wait_bounded(&pc_full[n % kPieces], (uint32_t)(n / kPieces & 1), abort_p, wait_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok) p = ring[n % kPieces];
+        return ok && p.steps > 0;
+    };
+    auto done = [&](int n) {
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&pc_empty[n % kPieces]);
+    };
     Piece pc;
     if (warp < 4) {
         ptx::setmaxnreg_dec<kCtrlRegs>();
-        if (warp == 0) {
+        if (warp == 2) {
+            // ============================== pieces ==============================
+            if (lane == 0) {
+                for (int n = 0;; ++n) {
+                    if (!ptx::mbar_wait_bounded(&pc_empty[n % kPieces], (uint32_t)(n / kPieces & 1) ^ 1u, abort_p, wait_limit)) {
+                        atomicOr(c.head + kCacheStatus, kDevTimeout);
+                        break;
+                    }
+                    const bool some = walk.next(pc, G, U);
+                    if (!some) pc.steps = 0;
+                    ring[n % kPieces] = pc;
+                    ptx::mbar_arrive(&pc_full[n % kPieces]);
+                    if (!some) break;
+                }
+            }
+        } else if (warp == 0) {
             // ============================= MMA issuer =============================
             constexpr uint32_t idS = ptx::idesc_f16(kTile, kTile, false, false);
             constexpr uint32_t idO = ptx::idesc_f16(kTile, D, false, true);
@@ -275,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ptx::mma_ss(tbase + t * 128, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
                 }
             };
-            while (ok && walk.next(pc)) {
+            while (piece(pieces, pc)) {
                 const int n = pc.b1 - pc.b0, T = pc.tiles;
                 ok = wait_all(&q_full, (uint32_t)(pieces & 1)) && wait_all(&k_full[nk % kK], (uint32_t)((nk / kK) & 1));
                 if (!ok) break;
@@ -321,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
                 if (!ok) break;
                 if (ptx::elect_one_sync()) ptx::mma_commit(&o_full);
-                __syncwarp();
+                done(pieces);
                 ++pieces;
             }
             if (!ok) {
@@ -344,23 +384,27 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const int chunk = x % (D / 32), tok = x % kPer / (D / 32), rec0 = x / kPer;
         constexpr int kRecStep = 128 / kPer;  // records per iteration
         uint4 kc[kIt], vc[kIt];
-        uint32_t ks[kIt], vs[kIt];  // f16 pairs of the two scales
-        int page[kIt];
+        uint32_t ks[kIt], vs[kIt], vs2[kIt];  // scales, as they were loaded: nothing here waits for a load
+        int page[kIt], page_next[kIt];
         // 16-byte slots of the unit's row: the order in which a lane writes them
         // keeps eight lanes' stores in eight different slots
         const int turn = D == 128 ? 2 * (chunk >> 1) : 0;
         const uint32_t row_base = (uint32_t)((chunk >> 1) * (kTile * 128)), slot0 = (uint32_t)((chunk & 1) * 4);
         Piece nx;
-        int j = 0;
-        bool have = walk.next(nx);
-        if (have) j = nx.b0;
+        int j = 0, pieces = 0;
+        bool have = piece(0, nx);
         auto record_of = [&](int i) { return 8 * j + rec0 + kRecStep * i; };
-        auto pages = [&]() {
-            const int* row = c.table + (size_t)(a.seqs ? a.seqs[nx.seq] : nx.seq) * c.W;
+        const int* row = c.table;  // of the piece's sequence
+        auto enter = [&]() {
+            if (!have) return;
+            j = nx.b0;
+            row = c.table + (size_t)(a.seqs ? a.seqs[nx.seq] : nx.seq) * c.W;
+        };
+        auto pages = [&](int (&p)[kIt], int step) {  // of a step of the piece, -1 past the sequence
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
-                const int r = record_of(i);
-                page[i] = 16 * r < nx.len ? row[r >> (c.log2_p - 4)] : -1;
+                const int r = 8 * step + rec0 + kRecStep * i;
+                p[i] = 16 * r < nx.len ? row[r >> (c.log2_p - 4)] : -1;
             }
         };
         auto base_of = [&](int i) {
@@ -383,13 +427,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
                 vc[i] = make_uint4(0u, 0u, 0u, 0u);
-                vs[i] = 0;
+                vs[i] = vs2[i] = 0;
                 // tokens past the sequence: zeros
                 if (cache_page_ok(c, page[i]) && 16 * record_of(i) + tok < nx.len) {
                     const uint8_t* p = base_of(i);
                     vc[i] = *reinterpret_cast<const uint4*>(p + cache_v_codes(D) + tok * (D / 2) + chunk * 16);
                     const uint8_t* q = p + cache_v_scales(D) + chunk * 32 + tok;
-                    vs[i] = q[0] | (uint32_t)q[16] << 8;
+                    vs[i] = q[0];
+                    vs2[i] = q[16];
                 }
             }
         };
@@ -420,8 +465,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar);
         };
+        enter();
         if (have) {
-            pages();
+            pages(page, j);
+            pages(page_next, j + 1);
             load_k();
             load_v();
         }
@@ -432,15 +479,23 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             give(&k_full[nk % kK]);
             ++nk;
             if (++j == nx.b1) {
-                have = walk.next(nx);
-                if (have) j = nx.b0;
+                done(pieces);
+                have = piece(++pieces, nx);
+                if (!ok) break;
+                enter();
+                if (have) pages(page, j);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kIt; ++i) page[i] = page_next[i];
             }
             if (have) {
-                pages();
                 load_k();
+                pages(page_next, j + 1);
             }
             ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&v_empty[nv % kV], (uint32_t)((nv / kV) & 1) ^ 1u, abort_p, wait_limit));
             if (!ok) break;
+#pragma unroll
+            for (int i = 0; i < kIt; ++i) vs[i] |= vs2[i] << 8;
             put(sV + (nv % kV) * C::kBytes, vc, vs);
             give(&v_full[nv % kV]);
             ++nv;
@@ -455,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
         const uint32_t tS = tbase + t * 128 + lane_off, tO = tbase + 256 + t * 128 + lane_off;
         int ns = 0, pieces = 0;
-        while (ok && walk.next(pc)) {
+        while (piece(pieces, pc)) {
             const int R = pc.blk * kBlock + t * kTile + r;  // row of (sequence, key head)
             const bool live = t * kTile + r < pc.rows;
             float f = 0.f;      // to base-2 scores
@@ -583,7 +638,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             }
             ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
             ok = ptx::named_bar_and(1, 256, ok);
-            ++pieces;
             if (!ok) break;
             ptx::tc_fence_after();
 
@@ -640,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             }
             ptx::tc_fence_before();
             if (!whole) {
-                const int first = cta_of(pc.item0), n = cta_of(pc.item0 + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
+                const int first = pc.first, n = pc.pieces;
                 ptx::named_bar_sync(1, 256);
                 if (threadIdx.x == 256) {
                     __threadfence();
@@ -683,6 +737,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     }
                 }
             }
+            done(pieces);
+            ++pieces;
         }
         if (!ok && lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
     }
