@@ -13,9 +13,10 @@
 //               (P from TMEM), f16 in fp32
 //   warp 1      TMEM (all 512 columns)
 //   warp 2      the CTA's pieces, into a ring that the others read
-//   warps 4-7   codes to f16: a step's codes and scales of K and then of V from
-//               global memory into registers, one step ahead; code times scale,
-//               which f16 holds exactly, into 128-byte-swizzled tiles
+//   warp 3      codes and scales of a step's keys, then values, into a ring: a
+//               bulk copy per record of 16 tokens
+//   warps 4-7   codes to f16: code times scale, which f16 holds exactly, from the
+//               ring into 128-byte-swizzled tiles
 //   warps 8-11  softmax of tile 0, warps 12-15 of tile 1: a thread per row. They
 //               also put Q into shared memory, as f16 with the row's largest value
 //               near 2^14 (the row's power of two joins the softmax scale)
@@ -41,18 +42,23 @@ namespace {
 constexpr int kTile = 128;  // rows of a tile, tokens of a step
 constexpr int kBlock = 2 * kTile;
 constexpr int kThreads = 512;
-constexpr int kK = 2, kV = 3;  // tiles of K and V in shared memory
+constexpr int kK = 2, kV = 2;  // tiles of K and V in shared memory
+constexpr int kMaxCodes = 8;   // half steps of codes (K's or V's) in flight
 constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
 constexpr float kLowest = -3.402823466e38f;
 // 128 registers a thread at launch, shared out anew.
-constexpr int kLaunchRegs = 128, kCtrlRegs = 56, kCodeRegs = 88, kSoftmaxRegs = 184;
+constexpr int kLaunchRegs = 128, kCtrlRegs = 56, kCodeRegs = 72, kSoftmaxRegs = 192;
 static_assert(4 * kCtrlRegs + 4 * kCodeRegs + 8 * kSoftmaxRegs <= 16 * kLaunchRegs, "register split");
 
 template <int D>
 struct ManyCfg {
     static constexpr int kBytes = kTile * D * 2;  // of a tile in shared memory
-    static constexpr int kUsed = (2 + kK + kV) * kBytes + 1024;
+    static constexpr int kCode = 8 * cache_v_codes(D);  // of a step's codes and scales of K, or of V
+    static constexpr int kCodes = D == 128 ? 3 : kMaxCodes;  // half steps that fit beside two tiles of Q
+    static constexpr int kUsed = (2 + kK + kV) * kBytes + kCodes * kCode + 1024;
     static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;  // one CTA per SM (all of TMEM)
+    // with one tile of Q its second is room for more
+    static constexpr int kCodes1 = kCodes + kBytes / kCode < kMaxCodes ? kCodes + kBytes / kCode : kMaxCodes;
     static constexpr size_t kSlot = (size_t)kBlock * (D + 2);  // floats of a partial result
 };
 static_assert(ManyCfg<128>::kSmem + 1024 <= 227 * 1024, "shared memory of the launch");
@@ -143,10 +149,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     using C = ManyCfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    unsigned char* sQ = smem;
-    unsigned char* sK = smem + 2 * C::kBytes;
+    unsigned char* sK = smem;
     unsigned char* sV = sK + kK * C::kBytes;
-    __shared__ uint64_t q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
+    unsigned char* sQ = sV + kV * C::kBytes;
+    const bool one_tile = a.group * a.queries <= kTile;
+    unsigned char* sC = sQ + (one_tile ? 1 : 2) * C::kBytes;
+    const int n_codes = one_tile ? C::kCodes1 : C::kCodes;
+    __shared__ uint64_t c_full[kMaxCodes], c_empty[kMaxCodes], q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
     __shared__ uint64_t s_full[2], p_full[2], o_full, drained;
     __shared__ uint64_t pc_full[kPieces], pc_empty[kPieces];
     __shared__ Piece ring[kPieces];
@@ -166,13 +175,17 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             ptx::mbar_init(&v_full[s], 4);
             ptx::mbar_init(&v_empty[s], 1);
         }
+        for (int s = 0; s < kMaxCodes; ++s) {
+            ptx::mbar_init(&c_full[s], 1);
+            ptx::mbar_init(&c_empty[s], 4);
+        }
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&s_full[t], 1);
             ptx::mbar_init(&p_full[t], 4);
         }
         for (int s = 0; s < kPieces; ++s) {
             ptx::mbar_init(&pc_full[s], 1);
-            ptx::mbar_init(&pc_empty[s], 13);  // warps that read pieces
+            ptx::mbar_init(&pc_empty[s], 14);  // warps that read pieces
         }
         ptx::mbar_init(&o_full, 1);
         ptx::mbar_init(&drained, 1);
@@ -294,6 +307,41 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     if (!some) break;
                 }
             }
+        } else if (warp == 3) {
+            // ============================== codes ==============================
+            int half = 0, pieces = 0;
+            while (ok && piece(pieces, pc)) {
+                const int* row = c.table + (size_t)(a.seqs ? a.seqs[pc.seq] : pc.seq) * c.W;
+                const uint8_t* from = c.pool + (long long)a.layer * c.pages * c.page_bytes +
+                                      (long long)pc.hk * (c.P / 16) * cache_record_bytes(D);
+                for (int j = pc.b0; j < pc.b1 && ok; ++j) {
+                    const int r = 8 * j + lane, n = min(8, (pc.len + 15) / 16 - 8 * j);
+                    const uint8_t* rec = from;
+                    if (lane < n) {
+                        const int page = row[r >> (c.log2_p - 4)];
+                        // a page number from outside is read as page 0, like any stale page
+                        rec += (cache_page_ok(c, page) ? page : 0) * c.page_bytes + (r & (c.P / 16 - 1)) * cache_record_bytes(D);
+                    }
+                    for (int v = 0; v < 2; ++v, ++half) {
+                        const int sl = half % n_codes;
+                        ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&c_empty[sl], (uint32_t)(half / n_codes & 1) ^ 1u, abort_p, wait_limit));
+                        if (!ok) break;
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(&c_full[sl], (uint32_t)(n * cache_v_codes(D)));
+                        __syncwarp();
+                        if (lane < n)
+                            ptx::bulk_load(sC + sl * C::kCode + lane * cache_v_codes(D), rec + v * cache_v_codes(D), cache_v_codes(D), &c_full[sl]);
+                    }
+                }
+                done(pieces);
+                ++pieces;
+            }
+            if (!ok) {
+                // every copy issued lands before its space goes
+                volatile int never = 0;
+                for (int i = max(0, half - n_codes); i < half; ++i)
+                    ptx::mbar_wait_bounded(&c_full[i % n_codes], (uint32_t)(i / n_codes & 1), &never, kWaitLimit);
+                if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
+            }
         } else if (warp == 0) {
             // ============================= MMA issuer =============================
             constexpr uint32_t idS = ptx::idesc_f16(kTile, kTile, false, false);
@@ -380,65 +428,40 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         // scales, 64 bytes of f16. Thread x of iteration i has unit 128 i + x of
         // the step: lanes read whole rows.
         constexpr int kIt = D / 32, kPer = 16 * (D / 32);  // iterations; units of a record
+        constexpr int kRecStep = 128 / kPer;               // records per iteration
         const int x = (int)threadIdx.x - 128;
         const int chunk = x % (D / 32), tok = x % kPer / (D / 32), rec0 = x / kPer;
-        constexpr int kRecStep = 128 / kPer;  // records per iteration
-        uint4 kc[kIt], vc[kIt];
-        uint32_t ks[kIt], vs[kIt], vs2[kIt];  // scales, as they were loaded: nothing here waits for a load
-        int page[kIt], page_next[kIt];
+        const uint32_t codes_at = rec0 * cache_v_codes(D) + tok * (D / 2) + chunk * 16;
+        const uint32_t ks_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + tok * (D / 16) + chunk * 2;
+        const uint32_t vs_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + chunk * 32 + tok;
         // 16-byte slots of the unit's row: the order in which a lane writes them
         // keeps eight lanes' stores in eight different slots
         const int turn = D == 128 ? 2 * (chunk >> 1) : 0;
         const uint32_t row_base = (uint32_t)((chunk >> 1) * (kTile * 128)), slot0 = (uint32_t)((chunk & 1) * 4);
-        Piece nx;
-        int j = 0, pieces = 0;
-        bool have = piece(0, nx);
-        auto record_of = [&](int i) { return 8 * j + rec0 + kRecStep * i; };
-        const int* row = c.table;  // of the piece's sequence
-        auto enter = [&]() {
-            if (!have) return;
-            j = nx.b0;
-            row = c.table + (size_t)(a.seqs ? a.seqs[nx.seq] : nx.seq) * c.W;
-        };
-        auto pages = [&](int (&p)[kIt], int step) {  // of a step of the piece, -1 past the sequence
+        int half = 0, n_tiles = 0, pieces = 0;
+        // Half a step: the codes in slot `half` of the ring to f16 in `tile`.
+        // left: tokens of the step that the sequence has (values past it: zeros).
+        auto convert = [&](unsigned char* tile, bool values, int left) {
+            const int sl = half % n_codes;
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&c_full[sl], (uint32_t)(half / n_codes & 1), abort_p, wait_limit));
+            if (!ok) return;
+            const unsigned char* src = sC + sl * C::kCode;
+            uint4 w[kIt];
+            uint32_t sc[kIt];
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
-                const int r = 8 * step + rec0 + kRecStep * i;
-                p[i] = 16 * r < nx.len ? row[r >> (c.log2_p - 4)] : -1;
-            }
-        };
-        auto base_of = [&](int i) {
-            return c.pool + ((long long)a.layer * c.pages + page[i]) * c.page_bytes +
-                   (long long)(nx.hk * (c.P / 16) + (record_of(i) & (c.P / 16 - 1))) * cache_record_bytes(D);
-        };
-        auto load_k = [&]() {
-#pragma unroll
-            for (int i = 0; i < kIt; ++i) {
-                kc[i] = make_uint4(0u, 0u, 0u, 0u);
-                ks[i] = 0;
-                if (cache_page_ok(c, page[i])) {
-                    const uint8_t* p = base_of(i);
-                    kc[i] = *reinterpret_cast<const uint4*>(p + tok * (D / 2) + chunk * 16);
-                    ks[i] = *reinterpret_cast<const uint16_t*>(p + cache_k_scales(D) + tok * (D / 16) + chunk * 2);
+                const unsigned char* rec = src + i * (kRecStep * cache_v_codes(D));
+                w[i] = *reinterpret_cast<const uint4*>(rec + codes_at);
+                if (values) {
+                    sc[i] = rec[vs_at] | (uint32_t)rec[vs_at + 16] << 8;
+                    if (16 * (rec0 + kRecStep * i) + tok >= left) sc[i] = 0;
+                } else {
+                    sc[i] = *reinterpret_cast<const uint16_t*>(rec + ks_at);
                 }
             }
-        };
-        auto load_v = [&]() {
-#pragma unroll
-            for (int i = 0; i < kIt; ++i) {
-                vc[i] = make_uint4(0u, 0u, 0u, 0u);
-                vs[i] = vs2[i] = 0;
-                // tokens past the sequence: zeros
-                if (cache_page_ok(c, page[i]) && 16 * record_of(i) + tok < nx.len) {
-                    const uint8_t* p = base_of(i);
-                    vc[i] = *reinterpret_cast<const uint4*>(p + cache_v_codes(D) + tok * (D / 2) + chunk * 16);
-                    const uint8_t* q = p + cache_v_scales(D) + chunk * 32 + tok;
-                    vs[i] = q[0];
-                    vs2[i] = q[16];
-                }
-            }
-        };
-        auto put = [&](unsigned char* tile, const uint4 (&w)[kIt], const uint32_t (&sc)[kIt]) {
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&c_empty[sl]);
+            ++half;
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
                 const int r = 16 * (rec0 + kRecStep * i) + tok;  // row of the tile
@@ -459,47 +482,32 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
             }
         };
-        int nk = 0, nv = 0;
+        auto room = [&](uint64_t* bar, uint32_t parity) {
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, parity ^ 1u, abort_p, wait_limit));
+            return ok;
+        };
         auto give = [&](uint64_t* bar) {
             ptx::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar);
         };
-        enter();
-        if (have) {
-            pages(page, j);
-            pages(page_next, j + 1);
-            load_k();
-            load_v();
-        }
-        while (have) {
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&k_empty[nk % kK], (uint32_t)((nk / kK) & 1) ^ 1u, abort_p, wait_limit));
-            if (!ok) break;
-            put(sK + (nk % kK) * C::kBytes, kc, ks);
-            give(&k_full[nk % kK]);
-            ++nk;
-            if (++j == nx.b1) {
-                done(pieces);
-                have = piece(++pieces, nx);
+        static_assert(kK == kV, "one count of tiles");
+        while (ok && piece(pieces, pc)) {
+            for (int j = pc.b0; j < pc.b1; ++j, ++n_tiles) {
+                const int st = n_tiles % kK;
+                const uint32_t par = (uint32_t)(n_tiles / kK & 1);
+                const int left = pc.len - j * kTile;
+                if (!room(&k_empty[st], par)) break;
+                convert(sK + st * C::kBytes, false, left);
                 if (!ok) break;
-                enter();
-                if (have) pages(page, j);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kIt; ++i) page[i] = page_next[i];
+                give(&k_full[st]);
+                if (!room(&v_empty[st], par)) break;
+                convert(sV + st * C::kBytes, true, left);
+                if (!ok) break;
+                give(&v_full[st]);
             }
-            if (have) {
-                load_k();
-                pages(page_next, j + 1);
-            }
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&v_empty[nv % kV], (uint32_t)((nv / kV) & 1) ^ 1u, abort_p, wait_limit));
-            if (!ok) break;
-#pragma unroll
-            for (int i = 0; i < kIt; ++i) vs[i] |= vs2[i] << 8;
-            put(sV + (nv % kV) * C::kBytes, vc, vs);
-            give(&v_full[nv % kV]);
-            ++nv;
-            if (have) load_v();
+            done(pieces);
+            ++pieces;
         }
         if (!ok && lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
     } else {
