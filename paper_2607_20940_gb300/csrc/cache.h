@@ -15,15 +15,23 @@ constexpr int kCacheBlock = 16;  // values that share a scale, and tokens of a r
 // A page of one layer is [Hk][P / 16] records of 16 tokens of a head, each
 //   key codes    [16 tokens][D / 2 bytes]   (two codes a byte, the lower dim in the lower half)
 //   key scales   [16 tokens][D / 16]
-//   value codes  [16 tokens][D / 2 bytes]
-//   value scales [D / 16][16 tokens]
-// so a warp's step over 16 tokens reads 18 D contiguous bytes (18 or 9 lines of
-// 128), keys' scales lie with their token (scores need a token's scales) and
-// values' with their block (outputs need a block's scales of several tokens).
+//   value codes  [16 tokens][D / 2 bytes], the 32-byte halves of a 64-byte row
+//                changed over for tokens 2, 3, 6, 7, ...
+//   value scales [D / 16][16 tokens, in the order of cache_v_scale_at]
+// so 16 tokens are 18 D contiguous bytes (18 or 9 lines of 128). Keys' scales lie
+// with their token and values' with their block, as the few-query kernel's
+// lanes need them; the orders among the tokens let its lanes read their rows
+// from shared memory without bank conflicts.
 __host__ __device__ constexpr int cache_record_bytes(int D) { return 18 * D; }
 __host__ __device__ constexpr int cache_k_scales(int D) { return 8 * D; }
 __host__ __device__ constexpr int cache_v_codes(int D) { return 9 * D; }
 __host__ __device__ constexpr int cache_v_scales(int D) { return 17 * D; }
+// Byte `at` of a token's value codes, within the token's row.
+__host__ __device__ constexpr int cache_v_code_at(int D, int token, int at) { return D == 128 ? at ^ (16 * (token & 2)) : at; }
+// A token's place among a block's 16 value scales: four lanes' tokens t, 4 + (t ^ 3), 8 + t, 12 + (t ^ 3) side by side.
+__host__ __device__ constexpr int cache_v_scale_at(int token) {
+    return 4 * ((token & 3) ^ (token & 4 ? 3 : 0)) + (token >> 2);
+}
 
 // Words of the state's header.
 enum : int { kCacheStatus = 0, kCacheCopies = 1, kCacheBad = 2, kCacheLive = 3 };

@@ -74,8 +74,8 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
             const float2 k = e2m1_f(rec[u * (D / 2) + at]);
             const float ks = e4m3_f(rec[cache_k_scales(D) + u * (D / 16) + blk]);
             z += (k.x * q[e][0] + k.y * q[e][1]) * ks;
-            v[e] = e2m1_f(rec[cache_v_codes(D) + u * (D / 2) + at]);
-            const float vs = e4m3_f(rec[cache_v_scales(D) + blk * 16 + u]);
+            v[e] = e2m1_f(rec[cache_v_codes(D) + u * (D / 2) + cache_v_code_at(D, u, at)]);
+            const float vs = e4m3_f(rec[cache_v_scales(D) + blk * 16 + cache_v_scale_at(u)]);
             v[e].x *= vs;
             v[e].y *= vs;
         }
@@ -139,22 +139,24 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // operations). A warp takes a record of 16 tokens at a time:
 //   scores [16 tokens x 8 rows] += K [16 x 16] Q^T, D / 16 products,
 //   out^T [16 dims x 8 rows] += V^T [16 x 16 tokens] P^T, D / 16 products,
-// mma.sync products of f16 in fp32: tcgen05 would need 64 rows, and the codes
-// would have to pass through shared memory. A code times its scale is exact in
-// f16. Which of a product's 16 columns stands for which dim or token is free,
-// so each lane keeps what it loads: 32 neighbouring dims of two tokens for the
-// scores, one block of four neighbouring tokens for the outputs, in whole
-// 64-byte rows per four and eight lanes. Two records are in flight per warp.
+// mma.sync products of f16 in fp32: tcgen05 would need 64 rows, and its f16
+// operands would have to pass through shared memory. A code times its scale is
+// exact in f16. Which of a product's 16 columns stands for which dim or token is
+// free, so each lane keeps what it loads: 32 neighbouring dims of two tokens for
+// the scores, one block of four tokens for the outputs. Records come through a
+// ring of bulk copies of the warp's own (no registers wait for memory).
 //
-// Work: every (sequence, key head) is cut into steps of 128 tokens (a record for
-// each of the eight warps); the CTAs take equal, contiguous shares of all steps.
-// A piece that is not a whole (sequence, head) leaves its unnormalised output,
-// maximum and sum in a slot, and the last CTA of it to finish adds the pieces in
-// order (the same bits whichever is last).
+// Work: every (sequence, key head) is an item of its records and kItem more units
+// (what a piece costs besides them); the warps of the grid take equal, contiguous
+// shares of all units, a CTA's warps neighbouring ones. A piece that is a whole item
+// is written by its warp. Others leave unnormalised output, maximum and sum in
+// shared memory; when the CTA's warps are done, each item's pieces are added in
+// order, and where an item goes over several CTAs, the last of them to finish
+// adds theirs in order (the same bits whichever is last).
 
-constexpr int kWarps = 8;
-constexpr int kStep = 16 * kWarps;  // tokens
 constexpr float kLowest = -3.402823466e38f;
+constexpr int kItem = 2;
+constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
 
 // c += a b, f16 in fp32.
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
@@ -168,12 +170,16 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     return r;
 }
 
-// What a lane holds of a record: lane 4 g + t.
+// The tokens of a record that stand in the products' rows 2 t, 2 t + 1, 8 + 2 t
+// and 9 + 2 t (cache_v_scale_at has the same order).
+__device__ __forceinline__ int token_of(int t, int e) { return 4 * e + (e & 1 ? t ^ 3 : t); }
+
+// What lane 4 g + t takes of a record.
 template <int D>
 struct Record {
-    uint32_t k[2][D / 32];  // tokens 4 (g / 2) + g % 2 and + 2: dims D / 4 t ...
+    uint32_t k[2][D / 32];  // tokens of rows g and g + 8: dims D / 4 t ...
     uint32_t ks[2];         // and their scales
-    uint32_t v[4][D / 64];  // tokens 4 t ...: dims D / 8 g ...
+    uint32_t v[4][D / 64];  // tokens of t: dims D / 8 g ...
     uint32_t vs;            // and their four scales
 };
 
@@ -194,7 +200,7 @@ template <int D>
 __device__ __forceinline__ void load_record(Record<D>& r, const uint8_t* rec, int g, int t) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int tok = 4 * (g / 2) + g % 2 + 2 * e;
+        const int tok = token_of(g / 2, g % 2 + 2 * e);
         load_words(r.k[e], rec + tok * (D / 2) + t * (D / 8));
         const uint8_t* s = rec + cache_k_scales(D) + tok * (D / 16) + t * (D / 64);
         if constexpr (D == 128)
@@ -203,7 +209,10 @@ __device__ __forceinline__ void load_record(Record<D>& r, const uint8_t* rec, in
             r.ks[e] = *s;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) load_words(r.v[e], rec + cache_v_codes(D) + (4 * t + e) * (D / 2) + g * (D / 16));
+    for (int e = 0; e < 4; ++e) {
+        const int tok = token_of(t, e);
+        load_words(r.v[e], rec + cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, g * (D / 16)));
+    }
     r.vs = *reinterpret_cast<const uint32_t*>(rec + cache_v_scales(D) + (D == 128 ? g : g / 2) * 16 + 4 * t);
 }
 
@@ -220,24 +229,50 @@ __device__ __forceinline__ void operand(uint32_t (&a)[4], uint32_t w0, uint32_t 
 template <int D, int NT>
 struct FewCfg {
     static constexpr int kRows = 8 * NT;
-    static constexpr int kPitch = D + 4;  // floats of a row of outputs in shared memory
-    static constexpr int kSmem = kWarps * kRows * kPitch * 4;
-    static constexpr int kSlot = kRows * (D + 2);  // floats of a piece's partial result
+    static constexpr int kWarps = NT == 1 ? 16 : 12;
+    static constexpr int kStages = 4;
+    static constexpr int kPitch = D + 4;                        // floats of a row of outputs in shared memory
+    static constexpr int kPart = kRows * (kPitch + 2) * 4;      // a piece's output, maxima and sums
+    static constexpr int kRing = kStages * cache_record_bytes(D);
+    static constexpr int kOwn = kRing > kPart ? kRing : kPart;  // the ring, and then the warp's last piece
+    static constexpr int kSmem = kWarps * (kOwn + kPart) + 128;
+    static constexpr int kSlot = kRows * (D + 2);               // floats of a CTA's partial result
 };
+static_assert(FewCfg<128, 1>::kSmem <= 226 * 1024 && FewCfg<128, 2>::kSmem <= 226 * 1024, "shared memory of the launch");
 
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
-    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_steps) {
+__global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
+    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_units, long long wait_limit) {
     using C = FewCfg<D, NT>;
-    constexpr int kT = 32 * kWarps;
-    extern __shared__ __align__(16) float so[];  // [warp][row][kPitch]
-    __shared__ float sm[kWarps][C::kRows], sl[kWarps][C::kRows];
-    __shared__ float sw[kWarps][C::kRows], s_own[C::kRows], s_other[C::kRows], sM[C::kRows], sL[C::kRows];
-    __shared__ long long s_scan[kWarps];
-    __shared__ long long s_found[2];
-    __shared__ int s_last;
+    constexpr int kW = C::kWarps, kT = 32 * kW, kS = C::kStages, kRec = cache_record_bytes(D);
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t full[kW][kS];
+    __shared__ float s_w[2][kW][C::kRows];                 // weights of the warps' first and last pieces
+    __shared__ float s_own[kW][C::kRows], s_other[kW][C::kRows];  // an item's join, by the warp that adds it
+    __shared__ float s_M[C::kRows];
+    __shared__ long long s_scan[kW], s_found[2];
+    // Pieces that are not whole items. first: the item began before the warp (2: and
+    // goes on after it); last: it begins in the warp and goes on.
+    __shared__ int s_first[kW], s_last[kW];
+    __shared__ int s_alone[kW][2];  // of a last piece whose item is this CTA's alone: row of the list, head
+    __shared__ int s_item[2][4];    // items of several CTAs, begun before this one and in it: row, head, first CTA, CTAs
+    __shared__ int s_merge[2];
+    __shared__ int abort_flag;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     const int rows = a.group * a.queries;
+    unsigned char* ring = smem + warp * C::kOwn;
+    auto part_of = [&](int w, int last) {  // the first piece of warp w, or its last
+        return reinterpret_cast<float*>(last ? smem + w * C::kOwn : smem + kW * C::kOwn + w * C::kPart);
+    };
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (threadIdx.x < 2) s_merge[threadIdx.x] = 0;
+    if (lane == 0) {
+        for (int s = 0; s < kS; ++s) ptx::mbar_init(&full[warp][s], 1);
+        ptx::fence_mbar_init();
+        s_first[warp] = s_last[warp] = 0;
+    }
+    __syncthreads();
+    volatile int* abort_p = &abort_flag;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
@@ -245,8 +280,9 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
         const int s = a.seqs ? a.seqs[i] : i;
         return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
     };
-    auto steps_of = [&](int len) { return (len + kStep - 1) / kStep; };
-    // Row r of (sequence i, key head hk): its place in q, out and lse.
+    auto records_of = [&](int len) { return (len + 15) / 16; };
+    auto units_of = [&](int len) { return len > 0 ? records_of(len) + kItem : 0; };
+    // Row r of (row i of the list, key head hk): its place in q, out and lse.
     auto place = [&](const long long* st, int i, int hk, int r) {
         return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
     };
@@ -266,7 +302,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
         long long before = 0;
         all = 0;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kW; ++w) {
             if (w < warp) before += s_scan[w];
             all += s_scan[w];
         }
@@ -291,64 +327,78 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
                 a.lse[lse_place(i, hk, r)] = a.base_lse ? a.base_lse[lse_place(i, hk, r)] : -INFINITY;
     }
 
-    // ---- this CTA's share of the steps, and the (sequence, head) it begins in
+    // ---- the warps' shares. A step belongs to the warp that has its unit: item's
+    // first + kItem + record; the CTA finds the sequence that its first warp begins in.
     long long U = 0, mine = 0;
-    for (int i = threadIdx.x; i < a.n; i += kT) mine += steps_of(length(i));
+    for (int i = threadIdx.x; i < a.n; i += kT) mine += units_of(length(i));
     scan(mine, U);
     U *= c.Hk;
-    const int G = (int)min((long long)gridDim.x, max(1ll, U / min_steps));
-    if ((int)blockIdx.x >= G) return;
-    const long long u0 = U * blockIdx.x / G, u1 = U * (blockIdx.x + 1) / G;
-    if (u0 >= u1) return;
-    auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
-    long long base = 0;
-    for (int i0 = 0; i0 < a.n; i0 += kT) {
-        const int i = i0 + (int)threadIdx.x;
-        const long long x = i < a.n ? (long long)steps_of(length(i)) * c.Hk : 0;
-        long long all;
-        const long long before = base + scan(x, all);
-        if (u0 >= before && u0 < before + x) {
-            s_found[0] = i;
-            s_found[1] = before;
+    const int workers = (int)min((long long)gridDim.x * kW, max(1ll, U / min_units));
+    if ((int)blockIdx.x * kW >= workers || U == 0) return;
+    auto share = [&](int w) { return w >= workers ? U : (long long)((unsigned long long)U * w / workers); };
+    auto worker_of = [&](long long u) { return (int)(((u + 1) * workers - 1) / U); };
+    const int me = (int)blockIdx.x * kW + warp;
+    const long long cta0 = share((int)blockIdx.x * kW);
+    {
+        long long base = 0;
+        for (int i0 = 0; i0 < a.n; i0 += kT) {
+            const int i = i0 + (int)threadIdx.x;
+            const long long x = i < a.n ? (long long)units_of(length(i)) * c.Hk : 0;
+            long long all;
+            const long long before = base + scan(x, all);
+            if (cta0 >= before && cta0 < before + x) {
+                s_found[0] = i;
+                s_found[1] = before;
+            }
+            base += all;
+            if (cta0 < base) break;
         }
-        base += all;
-        if (u0 < base) break;
+        __syncthreads();
     }
-    __syncthreads();
-    int seq = (int)s_found[0];
-    long long seq0 = s_found[1];  // first step of the sequence
 
-    for (long long u = u0; u < u1;) {
-        const int len = length(seq), n_steps = steps_of(len);
-        if (u >= seq0 + (long long)n_steps * c.Hk) {
-            seq0 += (long long)n_steps * c.Hk;
+    // ---- this warp's pieces
+    const long long u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
+    int seq = (int)s_found[0];
+    long long seq0 = s_found[1];  // first unit of the sequence
+    int issued = 0, taken = 0;    // records asked for and used, over all pieces
+    bool ok = true;
+    for (long long u = u0; u < u1 && ok;) {
+        const int len = length(seq), n_rec = records_of(len), per = units_of(len);
+        if (u >= seq0 + (long long)per * c.Hk) {
+            seq0 += (long long)per * c.Hk;
             ++seq;
             continue;
         }
-        const int hk = (int)((u - seq0) / n_steps);
-        const long long item0 = seq0 + (long long)hk * n_steps;
-        const int b0 = (int)(u - item0), b1 = (int)min((long long)n_steps, u1 - item0);
-        u = item0 + b1;
-        const int r_end = min((len + 15) / 16, b1 * kWarps);
+        const int hk = (int)((u - seq0) / per);
+        const long long item0 = seq0 + (long long)hk * per;
+        const int r0 = (int)max(0ll, u - item0 - kItem), r1 = (int)min((long long)n_rec, u1 - item0 - kItem);
+        u = item0 + per;
+        if (r0 >= r1) continue;  // the share ends before the first record, or began after the last
         const int* row = c.table + (size_t)(a.seqs ? a.seqs[seq] : seq) * c.W;
-        const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes +
-                              (long long)hk * (c.P / 16) * cache_record_bytes(D);
+        const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes + (long long)hk * (c.P / 16) * kRec;
         auto page_of = [&](int r) { return row[r >> (c.log2_p - 4)]; };
-        auto fetch = [&](Record<D>& x, int r, int page) {
-            // a page number from outside is read as page 0, like any stale page
-            const long long at = cache_page_ok(c, page) ? page : 0;
-            load_record<D>(x, pool + at * c.page_bytes + (r & (c.P / 16 - 1)) * cache_record_bytes(D), g, t);
+        auto fetch = [&](int r, int page) {
+            const int st = issued % kS;
+            ++issued;
+            if (lane == 0) {
+                // a page number from outside is read as page 0, like any stale page
+                const long long at = cache_page_ok(c, page) ? page : 0;
+                ptx::mbar_arrive_expect_tx(&full[warp][st], kRec);
+                ptx::bulk_load(ring + st * kRec, pool + at * c.page_bytes + (r & (c.P / 16 - 1)) * kRec, kRec, &full[warp][st]);
+            }
         };
-        Record<D> rec[2];
-        int r0 = b0 * kWarps + warp;
-        int page_next = 0;
-        if (r0 < r_end) fetch(rec[0], r0, page_of(r0));
-        if (r0 + kWarps < r_end) fetch(rec[1], r0 + kWarps, page_of(r0 + kWarps));
-        if (r0 + 2 * kWarps < r_end) page_next = page_of(r0 + 2 * kWarps);
+        int next = r0;  // record to ask for
+#pragma unroll
+        for (int s = 0; s < kS; ++s)
+            if (next < r1) {
+                fetch(next, page_of(next));
+                ++next;
+            }
+        int page_next = next < r1 ? page_of(next) : 0;
 
         // ---- queries: row g + 8 nt, dims D / 4 t ...
         uint32_t qf[NT][D / 16][2];
-        float f[NT][2];  // of rows 2 t and 2 t + 1: to base-2 scores
+        float f[NT][2];    // of rows 2 t and 2 t + 1: to base-2 scores
         int limit[NT][2];  // tokens that they see
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -383,7 +433,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
             for (int x = 0; x < 2; ++x) {
                 f[nt][x] = codes::row_factor(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x)), a.scale * c.k_unit);
                 const int rr = 8 * nt + 2 * t + x;
-                limit[nt][x] = rr >= rows ? 0 : a.causal ? len - a.queries + 1 + rr / a.group : len;
+                limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + rr / a.group : len;
             }
         }
         // no record below this one hides a token from a row
@@ -399,7 +449,13 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
         }
-        auto work = [&](Record<D>& x, int r) {
+        for (int r = r0; r < r1; ++r) {
+            const int st = taken % kS;
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp][st], (uint32_t)(taken / kS & 1), abort_p, wait_limit));
+            if (!ok) break;
+            ++taken;
+            Record<D> x;
+            load_record<D>(x, ring + st * kRec, g, t);
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
@@ -434,18 +490,17 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1];
             if (16 * r + 16 > all_see) {
-                const int tok = 16 * r + 4 * (g / 2) + g % 2;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (tok + (e & 2) >= limit[nt][e & 1]) s[nt][e] = -INFINITY;
+                        if (16 * r + token_of(g / 2, g % 2 + (e & 2)) >= min(limit[nt][e & 1], len)) s[nt][e] = -INFINITY;
                 // what lies past the sequence may be anything
-                const int left = len - 16 * r - 4 * t;
-                if (left < 1) vab &= 0xffff0000u;
-                if (left < 2) vab &= 0x0000ffffu;
-                if (left < 3) vcd &= 0xffff0000u;
-                if (left < 4) vcd &= 0x0000ffffu;
+                const int left = len - 16 * r;
+                if (token_of(t, 0) >= left) vab &= 0xffff0000u;
+                if (token_of(t, 1) >= left) vab &= 0x0000ffffu;
+                if (token_of(t, 2) >= left) vcd &= 0xffff0000u;
+                if (token_of(t, 3) >= left) vcd &= 0x0000ffffu;
             }
             // P is relative to a maximum that may lag the row's: with m five below
             // the maximum that it was taken from, P is 2^5 there and may grow to
@@ -507,23 +562,32 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 3], op, p[nt]);
             }
-        };
-        for (int r = r0; r < r_end; r += 2 * kWarps) {
-            work(rec[0], r);
-            if (r + 2 * kWarps < r_end) {
-                fetch(rec[0], r + 2 * kWarps, page_next);
-                if (r + 3 * kWarps < r_end) page_next = page_of(r + 3 * kWarps);
-            }
-            if (r + kWarps < r_end) {
-                work(rec[1], r + kWarps);
-                if (r + 3 * kWarps < r_end) {
-                    fetch(rec[1], r + 3 * kWarps, page_next);
-                    if (r + 4 * kWarps < r_end) page_next = page_of(r + 4 * kWarps);
-                }
+            // every lane has its part of the record
+            __syncwarp();
+            if (next < r1) {
+                fetch(next, page_next);
+                if (++next < r1) page_next = page_of(next);
             }
         }
+        if (!ok) break;
 
-        // ---- the warps' results together
+        // ---- the piece's result
+        const bool whole = r0 == 0 && r1 == n_rec;
+        float* part = part_of(warp, r0 == 0);
+        if (lane == 0 && !whole) {
+            if (r0 > 0)
+                s_first[warp] = r1 == n_rec ? 1 : 2;  // 2: goes on
+            else
+                s_last[warp] = 1;
+            // this CTA's items that other CTAs have too
+            const int first = worker_of(item0 + kItem) / kW, last = worker_of(item0 + kItem + n_rec - 1) / kW;
+            if (first < last) {
+                int* it = s_item[first < (int)blockIdx.x ? 0 : 1];
+                it[0] = seq, it[1] = hk, it[2] = first, it[3] = last - first + 1;
+            } else if (r0 == 0) {
+                s_alone[warp][0] = seq, s_alone[warp][1] = hk;
+            }
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -533,112 +597,161 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 2 : 1)
                 x += __shfl_xor_sync(0xffffffffu, x, 8);
                 x += __shfl_xor_sync(0xffffffffu, x, 16);
                 const int r = 8 * nt + 2 * t + e;
-                if (g == 0) {
-                    sm[warp][r] = m[nt][e];
-                    sl[warp][r] = x;
+                if (whole) {
+                    const bool live = r < rows;
+                    const long long at = live ? lse_place(seq, hk, r) : 0;
+                    const codes::Join j = codes::join_of(m[nt][e], x, a.base_lse != nullptr, a.base_lse && live ? a.base_lse[at] : 0.f, c.v_unit);
+                    __syncwarp();  // every lane has read base_lse, which may be lse
+                    if (live) {
+                        if (g == 0 && a.lse) a.lse[at] = j.lse;
+                        const long long out = place(a.o_st, seq, hk, r) + g * (D / 8);
+#pragma unroll
+                        for (int i = 0; i < D / 16; i += 4) {
+                            float y[8];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                y[2 * z] = o[nt][i + z][e] * j.own;
+                                y[2 * z + 1] = o[nt][i + z][e + 2] * j.own;
+                            }
+                            if (j.other != 0.f) {
+                                const uint4 b = *reinterpret_cast<const uint4*>(a.base_out + out + 2 * i);
+                                const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) {
+                                    y[2 * z] += j.other * codes::bf(bw[z] & 0xffffu);
+                                    y[2 * z + 1] += j.other * __uint_as_float(bw[z] & 0xffff0000u);
+                                }
+                            }
+                            *reinterpret_cast<uint4*>(a.out + out + 2 * i) =
+                                make_uint4(ptx::pack_bf16(y[0], y[1]), ptx::pack_bf16(y[2], y[3]), ptx::pack_bf16(y[4], y[5]),
+                                           ptx::pack_bf16(y[6], y[7]));
+                        }
+                    }
+                } else {
+                    if (g == 0) *reinterpret_cast<float2*>(part + C::kRows * C::kPitch + 2 * r) = make_float2(m[nt][e], x);
+                    float* dst = part + r * C::kPitch + g * (D / 8);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+                        *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[nt][i][e], o[nt][i][e + 2]);
                 }
-                float* dst = so + (warp * C::kRows + r) * C::kPitch + g * (D / 8);
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[nt][i][e], o[nt][i][e + 2]);
             }
-        __syncthreads();
-        const bool whole = b0 == 0 && b1 == n_steps;
-        if (threadIdx.x < C::kRows) {
-            const int r = threadIdx.x;
-            float M = kLowest, L = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][r]);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float x = codes::ex2(sm[w][r] - M);
-                sw[w][r] = x;
-                L += x * sl[w][r];
-            }
-            sM[r] = M;
-            sL[r] = L;
-            if (whole && r < rows) {
-                const long long at = lse_place(seq, hk, r);
-                const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
-                s_own[r] = j.own;
-                s_other[r] = j.other;
-                if (a.lse) a.lse[at] = j.lse;
-            }
+        __syncwarp();
+    }
+    if (!ok) {
+        // every copy asked for lands before its space goes
+        volatile int never = 0;
+        for (int i = taken; i < issued; ++i)
+            ptx::mbar_wait_bounded(&full[warp][i % kS], (uint32_t)(i / kS & 1), &never, kWaitLimit);
+        if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
+    }
+    if (__syncthreads_or(!ok)) return;
+
+    // ---- the CTA's pieces of an item, in order
+    auto store = [&](int i, int hk, int r, int d, float4 x, float own, float other) {  // four dims of a row's result
+        const long long at = place(a.o_st, i, hk, r) + d;
+        x.x *= own, x.y *= own, x.z *= own, x.w *= own;
+        if (other != 0.f) {
+            const uint2 y = *reinterpret_cast<const uint2*>(a.base_out + at);
+            x.x += other * codes::bf(y.x & 0xffffu), x.y += other * __uint_as_float(y.x & 0xffff0000u);
+            x.z += other * codes::bf(y.y & 0xffffu), x.w += other * __uint_as_float(y.y & 0xffff0000u);
         }
-        __syncthreads();
-        auto store = [&](int r, int d, float4 x) {  // four dims of a row's result
-            const long long at = place(a.o_st, seq, hk, r) + d;
-            const float own = s_own[r], other = s_other[r];
-            x.x *= own, x.y *= own, x.z *= own, x.w *= own;
-            if (other != 0.f) {
-                const uint2 y = *reinterpret_cast<const uint2*>(a.base_out + at);
-                x.x += other * codes::bf(y.x & 0xffffu), x.y += other * __uint_as_float(y.x & 0xffff0000u);
-                x.z += other * codes::bf(y.y & 0xffffu), x.w += other * __uint_as_float(y.y & 0xffff0000u);
-            }
-            *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(x.x, x.y), ptx::pack_bf16(x.z, x.w));
+        *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(x.x, x.y), ptx::pack_bf16(x.z, x.w));
+    };
+    auto finish = [&](int i, int hk, int r, float M, float L) {  // a row's join, by one thread
+        const long long at = lse_place(i, hk, r);
+        const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
+        if (a.lse) a.lse[at] = j.lse;
+        s_own[warp][r] = j.own;
+        s_other[warp][r] = j.other;
+    };
+    // The item whose pieces begin with warp w0's (its last, or the CTA's first).
+    auto combine = [&](int w0, int last) {
+        int end = w0, goes_on = last ? 1 : s_first[w0] == 2;
+        while (goes_on && end + 1 < kW) goes_on = s_first[++end] == 2;
+        const bool alone = last && !goes_on;  // else other CTAs have pieces too
+        auto ml_of = [&](int w, int r) {
+            return *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * r);
         };
-        float* slot = c.partials + (size_t)(2 * blockIdx.x + (b0 > 0 ? 0 : 1)) * C::kSlot;
-        for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
+        float* slot = c.partials + (size_t)(2 * blockIdx.x + last) * C::kSlot;
+        if (lane < rows) {
+            float M = kLowest, L = 0.f;
+            for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w, lane).x);
+            for (int w = w0; w <= end; ++w) {
+                const float2 x = ml_of(w, lane);
+                const float k = codes::ex2(x.x - M);
+                s_w[last && w == w0][w][lane] = k;
+                L += k * x.y;
+            }
+            if (alone)
+                finish(s_alone[w0][0], s_alone[w0][1], lane, M, L);
+            else
+                __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * lane), make_float2(M, L));
+        }
+        __syncwarp();
+        for (int x = lane; x < rows * (D / 4); x += 32) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float4 z = *reinterpret_cast<const float4*>(so + (w * C::kRows + r) * C::kPitch + d);
-                const float k = sw[w][r];
+            for (int w = w0; w <= end; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == w0) + r * C::kPitch + d);
+                const float k = s_w[last && w == w0][w][r];
                 y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
             }
-            if (whole)
-                store(r, d, y);
+            if (alone)
+                store(s_alone[w0][0], s_alone[w0][1], r, d, y, s_own[warp][r], s_other[warp][r]);
             else
                 __stcg(reinterpret_cast<float4*>(slot + r * D + d), y);
         }
-        if (!whole) {
-            if (threadIdx.x < rows)
-                __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * threadIdx.x), make_float2(sM[threadIdx.x], sL[threadIdx.x]));
-            const int first = cta_of(item0), pieces = cta_of(item0 + n_steps - 1) - first + 1;
-            __syncthreads();
-            if (threadIdx.x == 0) {
+        __syncwarp();
+        if (!alone && lane == 0) {
+            const int* it = s_item[last];
+            __threadfence();
+            s_merge[last] = atomicAdd(c.counters + it[2], 1u) == (unsigned)it[3] - 1;
+            if (s_merge[last]) {
+                c.counters[it[2]] = 0;  // for the next launch
                 __threadfence();
-                s_last = atomicAdd(c.counters + first, 1u) == (unsigned)pieces - 1;
-                if (s_last) {
-                    c.counters[first] = 0;  // for the next launch
-                    __threadfence();
-                }
-            }
-            __syncthreads();
-            if (s_last) {
-                // the piece of CTA first + k: its last share (slot 1) where the item begins in it, else slot 0
-                auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
-                if (threadIdx.x < rows) {
-                    const int r = threadIdx.x;
-                    float M = kLowest, L = 0.f;
-                    for (int k = 0; k < pieces; ++k) M = fmaxf(M, __ldcg(slot_of(k) + C::kRows * D + 2 * r));
-                    for (int k = 0; k < pieces; ++k) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(k) + C::kRows * D + 2 * r));
-                        L += codes::ex2(ml.x - M) * ml.y;
-                    }
-                    sM[r] = M;
-                    const long long at = lse_place(seq, hk, r);
-                    const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
-                    s_own[r] = j.own;
-                    s_other[r] = j.other;
-                    if (a.lse) a.lse[at] = j.lse;
-                }
-                __syncthreads();
-                for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
-                    const int r = x / (D / 4), d = x % (D / 4) * 4;
-                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int k = 0; k < pieces; ++k) {
-                        const float w = codes::ex2(__ldcg(slot_of(k) + C::kRows * D + 2 * r) - sM[r]);
-                        const float4 z = __ldcg(reinterpret_cast<const float4*>(slot_of(k) + r * D + d));
-                        y.x = fmaf(w, z.x, y.x), y.y = fmaf(w, z.y, y.y), y.z = fmaf(w, z.z, y.z), y.w = fmaf(w, z.w, y.w);
-                    }
-                    store(r, d, y);
-                }
             }
         }
-        __syncthreads();  // shared memory is free again
+    };
+    if (warp == 0 && s_first[0]) combine(0, 0);
+    if (s_last[warp]) combine(warp, 1);
+    __syncthreads();
+
+    // ---- items of several CTAs that this one finished last
+    for (int k = 0; k < 2; ++k) {
+        if (!s_merge[k]) continue;
+        const int i = s_item[k][0], hk = s_item[k][1], first = s_item[k][2], n = s_item[k][3];
+        // a CTA's piece of an item that begins in it is in its slot 1
+        auto slot_of = [&](int x) { return c.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * C::kSlot; };
+        for (int r = warp; r < rows; r += kW) {
+            float M = kLowest, L = 0.f;
+            for (int x = lane; x < n; x += 32) M = fmaxf(M, __ldcg(slot_of(x) + C::kRows * D + 2 * r));
+#pragma unroll
+            for (int d = 16; d; d /= 2) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+            for (int x = lane; x < n; x += 32) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(x) + C::kRows * D + 2 * r));
+                L += codes::ex2(ml.x - M) * ml.y;
+            }
+#pragma unroll
+            for (int d = 16; d; d /= 2) L += __shfl_xor_sync(0xffffffffu, L, d);
+            if (lane == 0) {
+                finish(i, hk, r, M, L);
+                s_M[r] = M;
+            }
+        }
+        __syncthreads();
+        for (int y = threadIdx.x; y < rows * (D / 4); y += kT) {
+            const int r = y / (D / 4), d = y % (D / 4) * 4;
+            const float M = s_M[r];
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int x = 0; x < n; ++x) {
+                const float w = codes::ex2(__ldcg(slot_of(x) + C::kRows * D + 2 * r) - M);
+                const float4 z = __ldcg(reinterpret_cast<const float4*>(slot_of(x) + r * D + d));
+                acc.x = fmaf(w, z.x, acc.x), acc.y = fmaf(w, z.y, acc.y), acc.z = fmaf(w, z.z, acc.z), acc.w = fmaf(w, z.w, acc.w);
+            }
+            store(i, hk, r, d, acc, s_own[r % kW][r], s_other[r % kW][r]);
+        }
+        __syncthreads();
     }
 }
 
@@ -649,9 +762,8 @@ cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t 
     cudaError_t e = device_sms(&sms);
     if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
     if (e != cudaSuccess) return e;
-    const int ctas = sms * (NT == 1 ? 2 : 1);
-    return launch_pdl(cache_few_kernel<D, NT>, dim3(ctas < kCacheMaxCtas ? ctas : kCacheMaxCtas), dim3(32 * kWarps), C::kSmem,
-                      st, c, a, 2);
+    return launch_pdl(cache_few_kernel<D, NT>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
+                      st, c, a, 4, kWaitLimit);
 }
 
 }  // namespace

@@ -433,7 +433,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const int chunk = x % (D / 32), tok = x % kPer / (D / 32), rec0 = x / kPer;
         const uint32_t codes_at = rec0 * cache_v_codes(D) + tok * (D / 2) + chunk * 16;
         const uint32_t ks_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + tok * (D / 16) + chunk * 2;
-        const uint32_t vs_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + chunk * 32 + tok;
+        const uint32_t v_at = rec0 * cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, chunk * 16);
+        const uint32_t vs_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + chunk * 32 + cache_v_scale_at(tok);
         // 16-byte slots of the unit's row: the order in which a lane writes them
         // keeps eight lanes' stores in eight different slots
         const int turn = D == 128 ? 2 * (chunk >> 1) : 0;
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
                 const unsigned char* rec = src + i * (kRecStep * cache_v_codes(D));
-                w[i] = *reinterpret_cast<const uint4*>(rec + codes_at);
+                w[i] = *reinterpret_cast<const uint4*>(rec + (values ? v_at : codes_at));
                 if (values) {
                     sc[i] = rec[vs_at] | (uint32_t)rec[vs_at + 16] << 8;
                     if (16 * (rec0 + kRecStep * i) + tok >= left) sc[i] = 0;
@@ -543,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const int e2 = codes::row_exponent(top);
                 const float up = codes::row_up(e2);
                 f = codes::row_factor(e2, a.scale * c.k_unit);
-                limit = !live ? 0 : a.causal ? pc.len - a.queries + 1 + R / a.group : pc.len;
+                limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + R / a.group : pc.len;
 #pragma unroll
                 for (int e = 0; e < D / 8; ++e) {
                     uint32_t y[4];
@@ -568,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4) ptx::tmem_ld32(tS + 32 * q4, s[q4]);
                     ptx::tmem_wait_ld();
-                    const int valid = limit - j * kTile;
+                    const int valid = min(limit, pc.len) - j * kTile;
                     if (valid < kTile) {
 #pragma unroll
                         for (int e = 0; e < 128; ++e)

@@ -55,8 +55,8 @@ __device__ __forceinline__ void block_at(const CacheView& c, int layer, int page
         codes = rec + t * (c.D / 2) + blk * 8;
         scale = rec + cache_k_scales(c.D) + t * (c.D / kCacheBlock) + blk;
     } else {
-        codes = rec + cache_v_codes(c.D) + t * (c.D / 2) + blk * 8;
-        scale = rec + cache_v_scales(c.D) + blk * kCacheBlock + t;
+        codes = rec + cache_v_codes(c.D) + t * (c.D / 2) + cache_v_code_at(c.D, t, blk * 8);
+        scale = rec + cache_v_scales(c.D) + blk * kCacheBlock + cache_v_scale_at(t);
     }
 }
 
