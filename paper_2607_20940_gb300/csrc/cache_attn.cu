@@ -136,17 +136,18 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 //
 // Up to 8 NT rows (the queries of the heads that share a key head) against a
 // sequence's tokens: bound by HBM (9/8 D bytes a token and key head, 4 D NT 8
-// operations). A warp takes a record of 16 tokens at a time:
+// operations), and close to it by the instructions that take codes apart. A warp
+// takes a pair of records (32 tokens) at a time; for each of them
 //   scores [16 tokens x 8 rows] += K [16 x 16] Q^T, D / 16 products,
 //   out^T [16 dims x 8 rows] += V^T [16 x 16 tokens] P^T, D / 16 products,
 // mma.sync products of f16 in fp32: tcgen05 would need 64 rows, and its f16
 // operands would have to pass through shared memory. A code times its scale is
 // exact in f16. Which of a product's 16 columns stands for which dim or token is
 // free, so each lane keeps what it loads: 32 neighbouring dims of two tokens for
-// the scores, one block of four tokens for the outputs. Records come through a
-// ring of bulk copies of the warp's own (no registers wait for memory).
+// the scores, one block of four tokens for the outputs. Pairs come through a ring
+// of bulk copies of the warp's own (no registers wait for memory).
 //
-// Work: every (sequence, key head) is an item of its records and kItem more units
+// Work: every (sequence, key head) is an item of its pairs and kItem more units
 // (what a piece costs besides them); the warps of the grid take equal, contiguous
 // shares of all units, a CTA's warps neighbouring ones. A piece that is a whole item
 // is written by its warp. Others leave unnormalised output, maximum and sum in
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // adds theirs in order (the same bits whichever is last).
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kItem = 2;
+constexpr int kItem = 1;
 constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
 
 // c += a b, f16 in fp32.
@@ -174,15 +175,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // and 9 + 2 t (cache_v_scale_at has the same order).
 __device__ __forceinline__ int token_of(int t, int e) { return 4 * e + (e & 1 ? t ^ 3 : t); }
 
-// What lane 4 g + t takes of a record.
-template <int D>
-struct Record {
-    uint32_t k[2][D / 32];  // tokens of rows g and g + 8: dims D / 4 t ...
-    uint32_t ks[2];         // and their scales
-    uint32_t v[4][D / 64];  // tokens of t: dims D / 8 g ...
-    uint32_t vs;            // and their four scales
-};
-
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&d)[N], const uint8_t* p) {
     if constexpr (N == 4) {
@@ -196,24 +188,30 @@ __device__ __forceinline__ void load_words(uint32_t (&d)[N], const uint8_t* p) {
     }
 }
 
+// What lane 4 g + t takes of a record: of the keys, dims D / 4 t ... of the tokens
+// of rows g and g + 8, and their scales; of the values, dims D / 8 g ... of the
+// four tokens of t, and their four scales.
 template <int D>
-__device__ __forceinline__ void load_record(Record<D>& r, const uint8_t* rec, int g, int t) {
+__device__ __forceinline__ void load_keys(uint32_t (&k)[2][D / 32], uint32_t (&ks)[2], const uint8_t* rec, int g, int t) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const int tok = token_of(g / 2, g % 2 + 2 * e);
-        load_words(r.k[e], rec + tok * (D / 2) + t * (D / 8));
+        load_words(k[e], rec + tok * (D / 2) + t * (D / 8));
         const uint8_t* s = rec + cache_k_scales(D) + tok * (D / 16) + t * (D / 64);
         if constexpr (D == 128)
-            r.ks[e] = *reinterpret_cast<const uint16_t*>(s);
+            ks[e] = *reinterpret_cast<const uint16_t*>(s);
         else
-            r.ks[e] = *s;
+            ks[e] = *s;
     }
+}
+template <int D>
+__device__ __forceinline__ void load_values(uint32_t (&v)[4][D / 64], uint32_t& vs, const uint8_t* rec, int g, int t) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int tok = token_of(t, e);
-        load_words(r.v[e], rec + cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, g * (D / 16)));
+        load_words(v[e], rec + cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, g * (D / 16)));
     }
-    r.vs = *reinterpret_cast<const uint32_t*>(rec + cache_v_scales(D) + (D == 128 ? g : g / 2) * 16 + 4 * t);
+    vs = *reinterpret_cast<const uint32_t*>(rec + cache_v_scales(D) + (D == 128 ? g : g / 2) * 16 + 4 * t);
 }
 
 // Byte J of four words as the product's f16 operand, times scales.
@@ -230,10 +228,10 @@ template <int D, int NT>
 struct FewCfg {
     static constexpr int kRows = 8 * NT;
     static constexpr int kWarps = NT == 1 ? 16 : 12;
-    static constexpr int kStages = 4;
+    static constexpr int kStages = 2;  // pairs of records in flight
     static constexpr int kPitch = D + 4;                        // floats of a row of outputs in shared memory
     static constexpr int kPart = kRows * (kPitch + 2) * 4;      // a piece's output, maxima and sums
-    static constexpr int kRing = kStages * cache_record_bytes(D);
+    static constexpr int kRing = 2 * kStages * cache_record_bytes(D);
     static constexpr int kOwn = kRing > kPart ? kRing : kPart;  // the ring, and then the warp's last piece
     static constexpr int kSmem = kWarps * (kOwn + kPart) + 128;
     static constexpr int kSlot = kRows * (D + 2);               // floats of a CTA's partial result
@@ -280,8 +278,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         const int s = a.seqs ? a.seqs[i] : i;
         return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
     };
-    auto records_of = [&](int len) { return (len + 15) / 16; };
-    auto units_of = [&](int len) { return len > 0 ? records_of(len) + kItem : 0; };
+    auto pairs_of = [&](int len) { return (len + 31) / 32; };
+    auto units_of = [&](int len) { return len > 0 ? pairs_of(len) + kItem : 0; };
     // Row r of (row i of the list, key head hk): its place in q, out and lse.
     auto place = [&](const long long* st, int i, int hk, int r) {
         return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
@@ -310,36 +308,49 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         return before + v - x;
     };
 
-    // ---- sequences without tokens: their rows are empty, or the base's
-    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk; x += gridDim.x) {
-        const int i = (int)(x / c.Hk), hk = (int)(x % c.Hk);
-        if (length(i) > 0) continue;
-        if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
-        for (int y = threadIdx.x; y < rows * (D / 8); y += kT) {
-            const int r = y / (D / 8), d = y % (D / 8) * 8;
-            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
-                w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
-            *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
-        }
-        if (a.lse && a.lse != a.base_lse)
-            for (int r = threadIdx.x; r < rows; r += kT)
-                a.lse[lse_place(i, hk, r)] = a.base_lse ? a.base_lse[lse_place(i, hk, r)] : -INFINITY;
-    }
-
-    // ---- the warps' shares. A step belongs to the warp that has its unit: item's
-    // first + kItem + record; the CTA finds the sequence that its first warp begins in.
+    // ---- all units, and those before each sequence of the first kT
     long long U = 0, mine = 0;
-    for (int i = threadIdx.x; i < a.n; i += kT) mine += units_of(length(i));
-    scan(mine, U);
+    bool none = false;
+    for (int i = threadIdx.x; i < a.n; i += kT) {
+        const int x = units_of(length(i));
+        none |= x == 0;
+        mine += x;
+    }
+    const long long before_mine = scan(mine, U) * c.Hk;
     U *= c.Hk;
+
+    // ---- sequences without tokens: their rows are empty, or the base's
+    if (__syncthreads_or(none))
+        for (long long x = blockIdx.x; x < (long long)a.n * c.Hk; x += gridDim.x) {
+            const int i = (int)(x / c.Hk), hk = (int)(x % c.Hk);
+            if (length(i) > 0) continue;
+            if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
+            for (int y = threadIdx.x; y < rows * (D / 8); y += kT) {
+                const int r = y / (D / 8), d = y % (D / 8) * 8;
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
+                    w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
+                *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+            }
+            if (a.lse && a.lse != a.base_lse)
+                for (int r = threadIdx.x; r < rows; r += kT)
+                    a.lse[lse_place(i, hk, r)] = a.base_lse ? a.base_lse[lse_place(i, hk, r)] : -INFINITY;
+        }
+
+    // ---- the warps' shares. A pair belongs to the warp that has its unit: the item's
+    // first + kItem + pair; the CTA finds the sequence that its first warp begins in.
     const int workers = (int)min((long long)gridDim.x * kW, max(1ll, U / min_units));
     if ((int)blockIdx.x * kW >= workers || U == 0) return;
     auto share = [&](int w) { return w >= workers ? U : (long long)((unsigned long long)U * w / workers); };
     auto worker_of = [&](long long u) { return (int)(((u + 1) * workers - 1) / U); };
     const int me = (int)blockIdx.x * kW + warp;
     const long long cta0 = share((int)blockIdx.x * kW);
-    {
+    if (a.n <= kT) {
+        if (cta0 >= before_mine && cta0 < before_mine + mine * c.Hk) {
+            s_found[0] = threadIdx.x;
+            s_found[1] = before_mine;
+        }
+    } else {
         long long base = 0;
         for (int i0 = 0; i0 < a.n; i0 += kT) {
             const int i = i0 + (int)threadIdx.x;
@@ -353,17 +364,17 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             base += all;
             if (cta0 < base) break;
         }
-        __syncthreads();
     }
+    __syncthreads();
 
     // ---- this warp's pieces
     const long long u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
     int seq = (int)s_found[0];
     long long seq0 = s_found[1];  // first unit of the sequence
-    int issued = 0, taken = 0;    // records asked for and used, over all pieces
+    int issued = 0, taken = 0;    // pairs asked for and used, over all pieces
     bool ok = true;
     for (long long u = u0; u < u1 && ok;) {
-        const int len = length(seq), n_rec = records_of(len), per = units_of(len);
+        const int len = length(seq), n_pairs = pairs_of(len), per = units_of(len);
         if (u >= seq0 + (long long)per * c.Hk) {
             seq0 += (long long)per * c.Hk;
             ++seq;
@@ -371,23 +382,26 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         }
         const int hk = (int)((u - seq0) / per);
         const long long item0 = seq0 + (long long)hk * per;
-        const int r0 = (int)max(0ll, u - item0 - kItem), r1 = (int)min((long long)n_rec, u1 - item0 - kItem);
+        const int r0 = (int)max(0ll, u - item0 - kItem), r1 = (int)min((long long)n_pairs, u1 - item0 - kItem);
         u = item0 + per;
-        if (r0 >= r1) continue;  // the share ends before the first record, or began after the last
+        if (r0 >= r1) continue;  // the share ends before the first pair
         const int* row = c.table + (size_t)(a.seqs ? a.seqs[seq] : seq) * c.W;
         const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes + (long long)hk * (c.P / 16) * kRec;
-        auto page_of = [&](int r) { return row[r >> (c.log2_p - 4)]; };
+        // Lanes 0 and 1 ask for a record of a pair each.
+        const int n_rec = (len + 15) / 16;
+        auto page_of = [&](int r) { return 2 * r + lane < n_rec && lane < 2 ? row[(2 * r + lane) >> (c.log2_p - 4)] : 0; };
         auto fetch = [&](int r, int page) {
-            const int st = issued % kS;
+            const int st = issued % kS, x = 2 * r + lane;
             ++issued;
-            if (lane == 0) {
+            if (lane == 0) ptx::mbar_arrive_expect_tx(&full[warp][st], (uint32_t)(min(2, n_rec - 2 * r) * kRec));
+            __syncwarp();
+            if (lane < 2 && x < n_rec) {
                 // a page number from outside is read as page 0, like any stale page
                 const long long at = cache_page_ok(c, page) ? page : 0;
-                ptx::mbar_arrive_expect_tx(&full[warp][st], kRec);
-                ptx::bulk_load(ring + st * kRec, pool + at * c.page_bytes + (r & (c.P / 16 - 1)) * kRec, kRec, &full[warp][st]);
+                ptx::bulk_load(ring + (2 * st + lane) * kRec, pool + at * c.page_bytes + (x & (c.P / 16 - 1)) * kRec, kRec, &full[warp][st]);
             }
         };
-        int next = r0;  // record to ask for
+        int next = r0;  // pair to ask for
 #pragma unroll
         for (int s = 0; s < kS; ++s)
             if (next < r1) {
@@ -436,7 +450,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + rr / a.group : len;
             }
         }
-        // no record below this one hides a token from a row
+        // no token below this one is hidden from a row
         const int all_see = a.causal ? max(0, len - a.queries + 1) : len;
 
         float o[NT][D / 16][4], m[NT][2], l[NT][2];
@@ -454,74 +468,78 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp][st], (uint32_t)(taken / kS & 1), abort_p, wait_limit));
             if (!ok) break;
             ++taken;
-            Record<D> x;
-            load_record<D>(x, ring + st * kRec, g, t);
-            float s[NT][4];
+            const uint8_t* pair = ring + 2 * st * kRec;
+            float s[2][NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-            {
-                const uint32_t k0 = codes::e4m3_f16x2(x.ks[0]), k1 = codes::e4m3_f16x2(x.ks[1]);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t k[2][D / 32], ks[2];
+                load_keys<D>(k, ks, pair + h * kRec, g, t);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[h][nt][0] = s[h][nt][1] = s[h][nt][2] = s[h][nt][3] = 0.f;
+                const uint32_t k0 = codes::e4m3_f16x2(ks[0]), k1 = codes::e4m3_f16x2(ks[1]);
                 auto part = [&](int wi, uint32_t s0, uint32_t s1) {  // words wi and wi + 1: a block of 16 dims
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const uint32_t w0 = x.k[0][wi + e], w1 = x.k[1][wi + e];
+                        const uint32_t w0 = k[0][wi + e], w1 = k[1][wi + e];
                         uint32_t op[4];
                         op[0] = codes::mul_f16x2(codes::e2m1_f16x2<0>(w0), s0);
                         op[1] = codes::mul_f16x2(codes::e2m1_f16x2<0>(w1), s1);
                         op[2] = codes::mul_f16x2(codes::e2m1_f16x2<1>(w0), s0);
                         op[3] = codes::mul_f16x2(codes::e2m1_f16x2<1>(w1), s1);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], op, qf[nt][2 * (wi + e)]);
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[h][nt], op, qf[nt][2 * (wi + e)]);
                         op[0] = codes::mul_f16x2(codes::e2m1_f16x2<2>(w0), s0);
                         op[1] = codes::mul_f16x2(codes::e2m1_f16x2<2>(w1), s1);
                         op[2] = codes::mul_f16x2(codes::e2m1_f16x2<3>(w0), s0);
                         op[3] = codes::mul_f16x2(codes::e2m1_f16x2<3>(w1), s1);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], op, qf[nt][2 * (wi + e) + 1]);
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[h][nt], op, qf[nt][2 * (wi + e) + 1]);
                     }
                 };
                 part(0, __byte_perm(k0, 0, 0x1010), __byte_perm(k1, 0, 0x1010));
                 if constexpr (D == 128) part(2, __byte_perm(k0, 0, 0x3232), __byte_perm(k1, 0, 0x3232));
             }
-            uint32_t vab = codes::e4m3_f16x2(x.vs & 0xffffu), vcd = codes::e4m3_f16x2(x.vs >> 16);
-            bool grew = false;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[nt][e] *= f[nt][e & 1];
-            if (16 * r + 16 > all_see) {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (16 * r + token_of(g / 2, g % 2 + (e & 2)) >= min(limit[nt][e & 1], len)) s[nt][e] = -INFINITY;
-                // what lies past the sequence may be anything
-                const int left = len - 16 * r;
-                if (token_of(t, 0) >= left) vab &= 0xffff0000u;
-                if (token_of(t, 1) >= left) vab &= 0x0000ffffu;
-                if (token_of(t, 2) >= left) vcd &= 0xffff0000u;
-                if (token_of(t, 3) >= left) vcd &= 0x0000ffffu;
+                    for (int e = 0; e < 4; ++e) s[h][nt][e] *= f[nt][e & 1];
+            const bool tail = 32 * r + 32 > all_see;
+            if (tail) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (32 * r + 16 * h + token_of(g / 2, g % 2 + (e & 2)) >= min(limit[nt][e & 1], len)) s[h][nt][e] = -INFINITY;
             }
             // P is relative to a maximum that may lag the row's: with m five below
             // the maximum that it was taken from, P is 2^5 there and may grow to
             // 2^15 before m follows. In f16, so P keeps its 11 bits down to 2^-19 of
             // the row's largest and is rounded to multiples of 2^-29 of it below.
+            float top[NT][2];
+            bool grew = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) grew |= s[nt][e] > m[nt][e & 1] + 15.f;
+                for (int e = 0; e < 2; ++e) {
+                    top[nt][e] = fmaxf(ptx::fmax3(s[0][nt][e], s[0][nt][e + 2], s[1][nt][e]), s[1][nt][e + 2]);
+                    grew |= top[nt][e] > m[nt][e] + 15.f;
+                }
             if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(s[nt][e], s[nt][e + 2]);
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                        top = fmaxf(top - 5.f, m[nt][e]);
-                        const float w = codes::ex2(m[nt][e] - top);
-                        m[nt][e] = top;
+                        float x = top[nt][e];
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        x = fmaxf(x - 5.f, m[nt][e]);
+                        const float w = codes::ex2(m[nt][e] - x);
+                        m[nt][e] = x;
                         l[nt][e] *= w;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
@@ -530,39 +548,54 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                         }
                     }
             }
-            uint32_t p[NT][2];
+            uint32_t p[2][NT][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float y[4];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = codes::ex2(s[nt][e] - m[nt][e & 1]);
-                l[nt][0] += y[0] + y[2];
-                l[nt][1] += y[1] + y[3];
-                p[nt][0] = transposed(codes::pack_f16(y[0], y[1]));
-                p[nt][1] = transposed(codes::pack_f16(y[2], y[3]));
+                for (int nt = 0; nt < NT; ++nt) {
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = codes::ex2(s[h][nt][e] - m[nt][e & 1]);
+                    l[nt][0] += y[0] + y[2];
+                    l[nt][1] += y[1] + y[3];
+                    p[h][nt][0] = transposed(codes::pack_f16(y[0], y[1]));
+                    p[h][nt][1] = transposed(codes::pack_f16(y[2], y[3]));
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v[4][D / 64], vs;
+                load_values<D>(v, vs, pair + h * kRec, g, t);
+                uint32_t vab = codes::e4m3_f16x2(vs & 0xffffu), vcd = codes::e4m3_f16x2(vs >> 16);
+                if (tail) {  // what lies past the sequence may be anything
+                    const int left = len - 32 * r - 16 * h;
+                    if (token_of(t, 0) >= left) vab &= 0xffff0000u;
+                    if (token_of(t, 1) >= left) vab &= 0x0000ffffu;
+                    if (token_of(t, 2) >= left) vcd &= 0xffff0000u;
+                    if (token_of(t, 3) >= left) vcd &= 0x0000ffffu;
+                }
+#pragma unroll
+                for (int w = 0; w < D / 64; ++w) {
+                    // a byte: the same dim of two tokens
+                    constexpr uint32_t kLow = 0x0f0f0f0fu;
+                    const uint32_t va = v[0][w], vb = v[1][w], vc = v[2][w], vd = v[3][w];
+                    const uint32_t ab0 = (va & kLow) | ((vb << 4) & ~kLow), ab1 = ((va >> 4) & kLow) | (vb & ~kLow);
+                    const uint32_t cd0 = (vc & kLow) | ((vd << 4) & ~kLow), cd1 = ((vc >> 4) & kLow) | (vd & ~kLow);
+                    uint32_t op[4];
+                    operand<0>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w], op, p[h][nt]);
+                    operand<1>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 1], op, p[h][nt]);
+                    operand<2>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 2], op, p[h][nt]);
+                    operand<3>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 3], op, p[h][nt]);
+                }
             }
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) {
-                // a byte: the same dim of two tokens
-                constexpr uint32_t kLow = 0x0f0f0f0fu;
-                const uint32_t va = x.v[0][w], vb = x.v[1][w], vc = x.v[2][w], vd = x.v[3][w];
-                const uint32_t ab0 = (va & kLow) | ((vb & kLow) << 4), ab1 = ((va >> 4) & kLow) | (vb & ~kLow);
-                const uint32_t cd0 = (vc & kLow) | ((vd & kLow) << 4), cd1 = ((vc >> 4) & kLow) | (vd & ~kLow);
-                uint32_t op[4];
-                operand<0>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w], op, p[nt]);
-                operand<1>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 1], op, p[nt]);
-                operand<2>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 2], op, p[nt]);
-                operand<3>(op, ab0, ab1, cd0, cd1, vab, vab, vcd, vcd);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + 3], op, p[nt]);
-            }
-            // every lane has its part of the record
+            // every lane has its part of the pair
             __syncwarp();
             if (next < r1) {
                 fetch(next, page_next);
@@ -572,15 +605,15 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         if (!ok) break;
 
         // ---- the piece's result
-        const bool whole = r0 == 0 && r1 == n_rec;
+        const bool whole = r0 == 0 && r1 == n_pairs;
         float* part = part_of(warp, r0 == 0);
         if (lane == 0 && !whole) {
             if (r0 > 0)
-                s_first[warp] = r1 == n_rec ? 1 : 2;  // 2: goes on
+                s_first[warp] = r1 == n_pairs ? 1 : 2;  // 2: goes on
             else
                 s_last[warp] = 1;
             // this CTA's items that other CTAs have too
-            const int first = worker_of(item0 + kItem) / kW, last = worker_of(item0 + kItem + n_rec - 1) / kW;
+            const int first = worker_of(item0 + kItem) / kW, last = worker_of(item0 + kItem + n_pairs - 1) / kW;
             if (first < last) {
                 int* it = s_item[first < (int)blockIdx.x ? 0 : 1];
                 it[0] = seq, it[1] = hk, it[2] = first, it[3] = last - first + 1;
@@ -664,56 +697,83 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         s_own[warp][r] = j.own;
         s_other[warp][r] = j.other;
     };
-    // The item whose pieces begin with warp w0's (its last, or the CTA's first).
-    auto combine = [&](int w0, int last) {
-        int end = w0, goes_on = last ? 1 : s_first[w0] == 2;
+    // An item's pieces begin with warp w0's last, or with the CTA's first; the others
+    // are the first pieces of the warps after it, up to `end`. Returns whether the
+    // item goes on in the next CTA.
+    auto extent = [&](int w0, int last, int& end) {
+        end = w0;
+        bool goes_on = last ? true : s_first[w0] == 2;
         while (goes_on && end + 1 < kW) goes_on = s_first[++end] == 2;
-        const bool alone = last && !goes_on;  // else other CTAs have pieces too
-        auto ml_of = [&](int w, int r) {
+        return goes_on;
+    };
+    // Row r's maximum and sum over them; their weights into s_w.
+    auto weigh = [&](int w0, int last, int end, int r, float& M, float& L) {
+        auto ml_of = [&](int w) {
             return *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * r);
         };
-        float* slot = c.partials + (size_t)(2 * blockIdx.x + last) * C::kSlot;
+        M = kLowest, L = 0.f;
+        for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w).x);
+        for (int w = w0; w <= end; ++w) {
+            const float2 x = ml_of(w);
+            const float k = codes::ex2(x.x - M);
+            s_w[last && w == w0][w][r] = k;
+            L += k * x.y;
+        }
+    };
+    auto sum = [&](int w0, int last, int end, int r, int d) {
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = w0; w <= end; ++w) {
+            const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == w0) + r * C::kPitch + d);
+            const float k = s_w[last && w == w0][w][r];
+            y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
+        }
+        return y;
+    };
+    // Items of this CTA alone: by the warp that has the first piece.
+    int end, over = -1;  // over: the warp whose last piece's item goes on in the next CTA
+    if (s_last[warp] && !extent(warp, 1, end)) {
+        const int i = s_alone[warp][0], hk = s_alone[warp][1];
         if (lane < rows) {
-            float M = kLowest, L = 0.f;
-            for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w, lane).x);
-            for (int w = w0; w <= end; ++w) {
-                const float2 x = ml_of(w, lane);
-                const float k = codes::ex2(x.x - M);
-                s_w[last && w == w0][w][lane] = k;
-                L += k * x.y;
-            }
-            if (alone)
-                finish(s_alone[w0][0], s_alone[w0][1], lane, M, L);
-            else
-                __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * lane), make_float2(M, L));
+            float M, L;
+            weigh(warp, 1, end, lane, M, L);
+            finish(i, hk, lane, M, L);
         }
         __syncwarp();
         for (int x = lane; x < rows * (D / 4); x += 32) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = w0; w <= end; ++w) {
-                const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == w0) + r * C::kPitch + d);
-                const float k = s_w[last && w == w0][w][r];
-                y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
-            }
-            if (alone)
-                store(s_alone[w0][0], s_alone[w0][1], r, d, y, s_own[warp][r], s_other[warp][r]);
-            else
-                __stcg(reinterpret_cast<float4*>(slot + r * D + d), y);
+            store(i, hk, r, d, sum(warp, 1, end, r, d), s_own[warp][r], s_other[warp][r]);
         }
         __syncwarp();
-        if (!alone && lane == 0) {
-            const int* it = s_item[last];
+    }
+    // Items of several CTAs: by the whole CTA, into its slots.
+    for (int w = 0; w < kW; ++w)
+        if (s_last[w] && extent(w, 1, end)) over = w;
+    for (int k = 0; k < 2; ++k) {
+        const int w0 = k ? over : s_first[0] ? 0 : -1;
+        if (w0 < 0) continue;
+        extent(w0, k, end);
+        float* slot = c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot;
+        if (threadIdx.x < rows) {
+            float M, L;
+            weigh(w0, k, end, threadIdx.x, M, L);
+            __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * threadIdx.x), make_float2(M, L));
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            __stcg(reinterpret_cast<float4*>(slot + r * D + d), sum(w0, k, end, r, d));
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int* it = s_item[k];
             __threadfence();
-            s_merge[last] = atomicAdd(c.counters + it[2], 1u) == (unsigned)it[3] - 1;
-            if (s_merge[last]) {
+            s_merge[k] = atomicAdd(c.counters + it[2], 1u) == (unsigned)it[3] - 1;
+            if (s_merge[k]) {
                 c.counters[it[2]] = 0;  // for the next launch
                 __threadfence();
             }
         }
-    };
-    if (warp == 0 && s_first[0]) combine(0, 0);
-    if (s_last[warp]) combine(warp, 1);
+    }
     __syncthreads();
 
     // ---- items of several CTAs that this one finished last
@@ -763,7 +823,7 @@ cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t 
     if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(cache_few_kernel<D, NT>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
-                      st, c, a, 4, kWaitLimit);
+                      st, c, a, 2, kWaitLimit);
 }
 
 }  // namespace
