@@ -30,6 +30,8 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache.h"
 #include "cache_codes.cuh"
 #include "internal.h"
@@ -425,24 +427,28 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         ptx::setmaxnreg_dec<kCodeRegs>();
         // ============================ codes to f16 ============================
         // A unit is 32 neighbouring dims of a token: 16 bytes of codes, two
-        // scales, 64 bytes of f16. Thread x of iteration i has unit 128 i + x of
-        // the step: lanes read whole rows.
-        constexpr int kIt = D / 32, kPer = 16 * (D / 32);  // iterations; units of a record
-        constexpr int kRecStep = 128 / kPer;               // records per iteration
+        // scales, 64 bytes of f16. A thread has the same token and dims of every
+        // kRecStep-th record. Eight lanes take four tokens and two chunks of 32
+        // dims, so that their 16-byte stores lie in eight different slots of the
+        // swizzled rows.
+        constexpr int kIt = D / 32, kPer = 16 * (D / 32);  // a thread's units of a step; units of a record
+        constexpr int kRecStep = 128 / kPer;               // records that the threads take at a time
         const int x = (int)threadIdx.x - 128;
-        const int chunk = x % (D / 32), tok = x % kPer / (D / 32), rec0 = x / kPer;
-        const uint32_t codes_at = rec0 * cache_v_codes(D) + tok * (D / 2) + chunk * 16;
+        const int chunk = (x & 1) + (D == 128 ? x >> 2 & 2 : 0);
+        const int rest = (x >> 1 & 3) + (D == 128 ? x >> 4 << 2 : x >> 3 << 2);  // token among kRecStep records'
+        const int tok = rest % 16, rec0 = rest / 16;
+        const uint32_t k_at = rec0 * cache_v_codes(D) + tok * (D / 2) + chunk * 16;
         const uint32_t ks_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + tok * (D / 16) + chunk * 2;
         const uint32_t v_at = rec0 * cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, chunk * 16);
         const uint32_t vs_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + chunk * 32 + cache_v_scale_at(tok);
-        // 16-byte slots of the unit's row: the order in which a lane writes them
-        // keeps eight lanes' stores in eight different slots
-        const int turn = D == 128 ? 2 * (chunk >> 1) : 0;
-        const uint32_t row_base = (uint32_t)((chunk >> 1) * (kTile * 128)), slot0 = (uint32_t)((chunk & 1) * 4);
+        const int row0 = 16 * rec0 + tok;  // of the tile; the next is 16 kRecStep rows on
+        const uint32_t tile_at = (uint32_t)((chunk >> 1) * (kTile * 128) + row0 * 128);
+        const uint32_t slot = (uint32_t)(((chunk & 1) * 4) ^ (row0 & 7)) << 4;
         int half = 0, n_tiles = 0, pieces = 0;
         // Half a step: the codes in slot `half` of the ring to f16 in `tile`.
         // left: tokens of the step that the sequence has (values past it: zeros).
-        auto convert = [&](unsigned char* tile, bool values, int left) {
+        auto convert = [&](unsigned char* tile, auto values, int left) {
+            constexpr bool kValues = decltype(values)::value;
             const int sl = half % n_codes;
             ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&c_full[sl], (uint32_t)(half / n_codes & 1), abort_p, wait_limit));
             if (!ok) return;
@@ -452,34 +458,35 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
                 const unsigned char* rec = src + i * (kRecStep * cache_v_codes(D));
-                w[i] = *reinterpret_cast<const uint4*>(rec + (values ? v_at : codes_at));
-                if (values) {
+                w[i] = *reinterpret_cast<const uint4*>(rec + (kValues ? v_at : k_at));
+                if constexpr (kValues)
                     sc[i] = rec[vs_at] | (uint32_t)rec[vs_at + 16] << 8;
-                    if (16 * (rec0 + kRecStep * i) + tok >= left) sc[i] = 0;
-                } else {
+                else
                     sc[i] = *reinterpret_cast<const uint16_t*>(rec + ks_at);
-                }
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&c_empty[sl]);
             ++half;
+            if (kValues && left < kTile) {
+#pragma unroll
+                for (int i = 0; i < kIt; ++i)
+                    if (row0 + 16 * kRecStep * i >= left) sc[i] = 0;
+            }
+            unsigned char* to = tile + tile_at;
 #pragma unroll
             for (int i = 0; i < kIt; ++i) {
-                const int r = 16 * (rec0 + kRecStep * i) + tok;  // row of the tile
                 const uint32_t two = codes::e4m3_f16x2(sc[i]);
                 const uint32_t s0 = __byte_perm(two, 0, 0x1010), s1 = __byte_perm(two, 0, 0x3232);
                 const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                unsigned char* row = tile + row_base + r * 128;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    // the slot's number within the unit depends on the lane, so the word is selected, not indexed
-                    const uint32_t y = turn ? cw[q ^ 2] : cw[q], s = (q ^ turn) < 2 ? s0 : s1;
+                    const uint32_t sq = q < 2 ? s0 : s1;
                     uint4 o;
-                    o.x = codes::mul_f16x2(codes::e2m1_f16x2<0>(y), s);
-                    o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(y), s);
-                    o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(y), s);
-                    o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(y), s);
-                    *reinterpret_cast<uint4*>(row + (((slot0 + (q ^ turn)) ^ (r & 7)) << 4)) = o;
+                    o.x = codes::mul_f16x2(codes::e2m1_f16x2<0>(cw[q]), sq);
+                    o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(cw[q]), sq);
+                    o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(cw[q]), sq);
+                    o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(cw[q]), sq);
+                    *reinterpret_cast<uint4*>(to + (slot ^ (uint32_t)(q << 4)) + i * (16 * kRecStep * 128)) = o;
                 }
             }
         };
@@ -499,11 +506,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const uint32_t par = (uint32_t)(n_tiles / kK & 1);
                 const int left = pc.len - j * kTile;
                 if (!room(&k_empty[st], par)) break;
-                convert(sK + st * C::kBytes, false, left);
+                convert(sK + st * C::kBytes, std::false_type{}, left);
                 if (!ok) break;
                 give(&k_full[st]);
                 if (!room(&v_empty[st], par)) break;
-                convert(sV + st * C::kBytes, true, left);
+                convert(sV + st * C::kBytes, std::true_type{}, left);
                 if (!ok) break;
                 give(&v_full[st]);
             }
