@@ -49,7 +49,7 @@ constexpr int kMaxCodes = 8;   // half steps of codes (K's or V's) in flight
 constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
 constexpr float kLowest = -3.402823466e38f;
 // 128 registers a thread at launch, shared out anew.
-constexpr int kLaunchRegs = 128, kCtrlRegs = 56, kCodeRegs = 72, kSoftmaxRegs = 192;
+constexpr int kLaunchRegs = 128, kCtrlRegs = 80, kCodeRegs = 64, kSoftmaxRegs = 184;
 static_assert(4 * kCtrlRegs + 4 * kCodeRegs + 8 * kSoftmaxRegs <= 16 * kLaunchRegs, "register split");
 
 template <int D>
@@ -73,19 +73,16 @@ struct Piece {
     int len;            // of the sequence
     int rows, tiles;    // of the block
     int steps, b0, b1;  // of the item; this piece's. steps 0: no more
-    int first, pieces;  // the CTAs that have the item
+    int item0;          // the item's first unit, from the CTA's first
 };
 constexpr int kPieces = 4;
 
-struct Walk {
+struct Shape {
     const CacheView& c;
     const CacheAttnArgs& a;
     int rows, blocks;
-    long long u0, u1;  // this CTA's units
-    int seq, hk, blk, len;
-    long long at;  // first unit of the next item
 
-    __device__ Walk(const CacheView& c_, const CacheAttnArgs& a_)
+    __device__ Shape(const CacheView& c_, const CacheAttnArgs& a_)
         : c(c_), a(a_), rows(a_.group * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
     __device__ int length(int i) const {
         const int s = a.seqs ? a.seqs[i] : i;
@@ -97,52 +94,12 @@ struct Walk {
         if (a.causal) n = min(n, max(0, n - a.queries + 1 + (b * kBlock + block_rows(b) - 1) / a.group));
         return (n + kTile - 1) / kTile;
     }
+    // Units (steps of one tile) of a key head of a sequence of n tokens.
     __device__ long long head_units(int n) const {
         if (!a.causal) return (long long)((n + kTile - 1) / kTile) * ((rows + kTile - 1) / kTile);
         long long u = 0;
         for (int b = 0; b < blocks; ++b) u += (long long)steps(n, b) * tiles(b);
         return u;
-    }
-    // Begin in sequence `i`, whose first unit is `first`.
-    __device__ void begin(int i, long long first, long long u0_, long long u1_) {
-        u0 = u0_, u1 = u1_;
-        seq = i;
-        len = length(i);
-        const long long per = head_units(len);
-        hk = (int)((u0 - first) / per);
-        at = first + hk * per;
-        blk = 0;
-    }
-    __device__ bool next(Piece& p, int G, long long U) {
-        auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
-        while (at < u1) {
-            const int n = steps(len, blk), w = tiles(blk);
-            const long long first = at;
-            p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
-            p.rows = block_rows(blk), p.tiles = w, p.steps = n;
-            at += (long long)n * w;
-            // step k belongs to the CTA that has unit first + k w
-            p.b0 = (int)min((long long)n, max(0ll, (u0 - first + w - 1) / w));
-            if (u0 <= first) p.b0 = 0;
-            p.b1 = (int)min((long long)n, (u1 - first + w - 1) / w);
-            const bool take = p.b0 < p.b1;
-            if (take) {
-                p.first = cta_of(first);
-                p.pieces = cta_of(first + (long long)(n - 1) * w) - p.first + 1;
-            }
-            if (++blk == blocks) {
-                blk = 0;
-                if (++hk == c.Hk) {
-                    hk = 0;
-                    if (at < u1) {
-                        do len = length(++seq);
-                        while (len == 0);
-                    }
-                }
-            }
-            if (take) return true;
-        }
-        return false;
     }
 };
 
@@ -205,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
-    Walk walk(c, a);
+    const Shape shape(c, a);
     auto place = [&](const long long* st, int i, int hk, int r) {
         return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
     };
@@ -214,11 +171,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     };
 
     // ---- blocks that see no token: their rows are empty, or the base's
-    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * walk.blocks; x += gridDim.x) {
-        const int b = (int)(x % walk.blocks), hk = (int)(x / walk.blocks % c.Hk), i = (int)(x / walk.blocks / c.Hk);
-        if (walk.steps(walk.length(i), b) > 0) continue;
+    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * shape.blocks; x += gridDim.x) {
+        const int b = (int)(x % shape.blocks), hk = (int)(x / shape.blocks % c.Hk), i = (int)(x / shape.blocks / c.Hk);
+        if (shape.steps(shape.length(i), b) > 0) continue;
         if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
-        const int n = walk.block_rows(b);
+        const int n = shape.block_rows(b);
         for (int y = threadIdx.x; y < n * (D / 8); y += kThreads) {
             const int r = b * kBlock + y / (D / 8), d = y % (D / 8) * 8;
             uint4 w = make_uint4(0u, 0u, 0u, 0u);
@@ -253,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         return before + v - x;
     };
     long long U = 0, mine = 0;
-    for (int i = threadIdx.x; i < a.n; i += kThreads) mine += walk.head_units(walk.length(i));
+    for (int i = threadIdx.x; i < a.n; i += kThreads) mine += shape.head_units(shape.length(i));
     scan(mine, U);
     U *= c.Hk;
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
@@ -263,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         long long base = 0;
         for (int i0 = 0; i0 < a.n; i0 += kThreads) {
             const int i = i0 + (int)threadIdx.x;
-            const long long x = i < a.n ? walk.head_units(walk.length(i)) * c.Hk : 0;
+            const long long x = i < a.n ? shape.head_units(shape.length(i)) * c.Hk : 0;
             long long all;
             const long long before = base + scan(x, all);
             if (u0 >= before && u0 < before + x) {
@@ -273,11 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             base += all;
             if (u0 < base) break;
         }
-        __syncthreads();
-        walk.begin((int)s_found[0], s_found[1], u0, u1);
-    } else {
-        walk.at = walk.u1 = 0;  // no pieces
     }
+    __syncthreads();
 
     bool ok = true;
     // The readers' side of the ring: the n-th piece, and that a warp is done with it.
@@ -297,14 +251,44 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         if (warp == 2) {
             // ============================== pieces ==============================
             if (lane == 0) {
+                // All from this CTA's first unit. The head that the share begins in
+                // may begin before it.
+                const int end = (int)(u1 - u0);
+                int seq = 0, hk = 0, blk = 0, len = 0, at = 0;
+                if (end > 0) {
+                    seq = (int)s_found[0];
+                    len = shape.length(seq);
+                    const long long per = shape.head_units(len);
+                    hk = (int)((u0 - s_found[1]) / per);
+                    at = (int)(s_found[1] + hk * per - u0);
+                }
                 for (int n = 0;; ++n) {
                     if (!ptx::mbar_wait_bounded(&pc_empty[n % kPieces], (uint32_t)(n / kPieces & 1) ^ 1u, abort_p, wait_limit)) {
                         atomicOr(c.head + kCacheStatus, kDevTimeout);
                         break;
                     }
-                    const bool some = walk.next(pc, G, U);
-                    if (!some) pc.steps = 0;
-                    ring[n % kPieces] = pc;
+                    Piece& p = ring[n % kPieces];
+                    p.steps = 0;
+                    while (at < end && p.steps == 0) {
+                        const int steps = shape.steps(len, blk), w = shape.tiles(blk);
+                        // step k belongs to the CTA that has unit at + k w
+                        const int b0 = at < 0 ? min(steps, (-at + w - 1) / w) : 0, b1 = min(steps, (end - at + w - 1) / w);
+                        if (b0 < b1) {
+                            p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
+                            p.rows = shape.block_rows(blk), p.tiles = w, p.steps = steps;
+                            p.b0 = b0, p.b1 = b1, p.item0 = at;
+                        }
+                        at += steps * w;
+                        if (++blk == shape.blocks) {
+                            blk = 0;
+                            if (++hk == c.Hk) {
+                                hk = 0;
+                                while (at < end && (len = shape.length(++seq)) == 0) {
+                                }
+                            }
+                        }
+                    }
+                    const bool some = p.steps > 0;
                     ptx::mbar_arrive(&pc_full[n % kPieces]);
                     if (!some) break;
                 }
@@ -352,62 +336,81 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             const uint64_t q_desc = ptx::sdesc_sw128(ptx::smem_u32(sQ), 16, 1024);
             const uint64_t k_desc = ptx::sdesc_sw128(ptx::smem_u32(sK), 16, 1024);
             const uint64_t v_desc = ptx::sdesc_sw128(ptx::smem_u32(sV), kTile * 128, 1024);
-            int nk = 0, nv = 0, pieces = 0, np[2] = {0, 0};
             auto wait_all = [&](uint64_t* bar, uint32_t parity) {
                 const bool r = ptx::mbar_wait_bounded(bar, parity, abort_p, wait_limit);
                 return __all_sync(0xffffffffu, r);
             };
-            auto scores = [&](int t) {  // S_t = Q_t K^T, K the tile nk
-                const uint64_t kd = k_desc + (uint64_t)(nk % kK) * kTileDesc, qd = q_desc + (uint64_t)t * kTileDesc;
+            auto issue_s = [&](int t, int st) {  // S_t = Q_t K^T
+                const uint64_t kd = k_desc + (uint64_t)st * kTileDesc, qd = q_desc + (uint64_t)t * kTileDesc;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint64_t off = (uint64_t)(((kk / 4) * (kTile * 128) + (kk % 4) * 32) >> 4);
                     ptx::mma_ss(tbase + t * 128, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
                 }
+                ptx::mma_commit(&s_full[t]);
             };
+            auto issue_o = [&](int t, int st, bool more) {  // O_t += P_t V
+                const uint64_t vd = v_desc + (uint64_t)st * kTileDesc;
+#pragma unroll
+                for (int kk = 0; kk < kTile / 16; ++kk)
+                    ptx::mma_ts(tbase + 256 + t * 128, tbase + t * 128 + kk * 8, vd + (uint64_t)(kk * (2048 >> 4)), idO,
+                                (more || kk > 0) ? 1u : 0u);
+            };
+            static_assert(kK == 2 && kV == 2, "slots take turns");
+            // Slots and phases of the next K and V tile and of each P.
+            int pieces = 0, st = 0;
+            uint32_t ph = 0, p_ph0 = 0, p_ph1 = 0;
             while (piece(pieces, pc)) {
-                const int n = pc.b1 - pc.b0, T = pc.tiles;
-                ok = wait_all(&q_full, (uint32_t)(pieces & 1)) && wait_all(&k_full[nk % kK], (uint32_t)((nk / kK) & 1));
+                const int n = pc.b1 - pc.b0;
+                const bool two = pc.tiles == 2;
+                ok = wait_all(&q_full, (uint32_t)(pieces & 1)) && wait_all(&k_full[st], ph);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 if (ptx::elect_one_sync()) {
-                    for (int t = 0; t < T; ++t) {
-                        scores(t);
-                        ptx::mma_commit(&s_full[t]);
-                    }
-                    ptx::mma_commit(&k_empty[nk % kK]);
+                    issue_s(0, st);
+                    if (two) issue_s(1, st);
+                    ptx::mma_commit(&k_empty[st]);
                 }
                 __syncwarp();
-                ++nk;
-                for (int j = 0; j < n && ok; ++j) {
+                for (int j = 0; j < n; ++j) {
                     const bool more = j + 1 < n;
-                    const int vs = nv % kV;
-                    ok = wait_all(&v_full[vs], (uint32_t)((nv / kV) & 1)) &&
-                         (!more || wait_all(&k_full[nk % kK], (uint32_t)((nk / kK) & 1)));
-                    for (int t = 0; t < T && ok; ++t) {
-                        ok = wait_all(&p_full[t], (uint32_t)(np[t] & 1));
+                    const int st1 = st ^ 1;
+                    const uint32_t ph1 = st1 == 0 ? ph ^ 1u : ph;
+                    // V of this step, K of the next and P0 of this: probed together
+                    {
+                        const bool rv = ptx::mbar_try_wait(&v_full[st], ph);
+                        const bool rk = !more || ptx::mbar_try_wait(&k_full[st1], ph1);
+                        const bool rp = ptx::mbar_try_wait(&p_full[0], p_ph0);
+                        if (!__all_sync(0xffffffffu, rv && rk && rp))
+                            ok = wait_all(&v_full[st], ph) && (!more || wait_all(&k_full[st1], ph1)) && wait_all(&p_full[0], p_ph0);
+                    }
+                    if (!ok) break;
+                    p_ph0 ^= 1u;
+                    ptx::tc_fence_after();
+                    if (ptx::elect_one_sync()) {
+                        issue_o(0, st, j > 0);
+                        if (more) issue_s(0, st1);
+                        if (!two) {
+                            ptx::mma_commit(&v_empty[st]);
+                            if (more) ptx::mma_commit(&k_empty[st1]);
+                        }
+                    }
+                    __syncwarp();
+                    if (two) {
+                        ok = wait_all(&p_full[1], p_ph1);
                         if (!ok) break;
-                        ++np[t];
+                        p_ph1 ^= 1u;
                         ptx::tc_fence_after();
                         if (ptx::elect_one_sync()) {
-                            const uint64_t vd = v_desc + (uint64_t)vs * kTileDesc;
-#pragma unroll
-                            for (int kk = 0; kk < kTile / 16; ++kk)
-                                ptx::mma_ts(tbase + 256 + t * 128, tbase + t * 128 + kk * 8, vd + (uint64_t)(kk * (2048 >> 4)),
-                                            idO, (j > 0 || kk > 0) ? 1u : 0u);
-                            if (more) {
-                                scores(t);
-                                ptx::mma_commit(&s_full[t]);
-                            }
-                            if (t == T - 1) {
-                                ptx::mma_commit(&v_empty[vs]);
-                                if (more) ptx::mma_commit(&k_empty[nk % kK]);
-                            }
+                            issue_o(1, st, j > 0);
+                            if (more) issue_s(1, st1);
+                            ptx::mma_commit(&v_empty[st]);
+                            if (more) ptx::mma_commit(&k_empty[st1]);
                         }
                         __syncwarp();
                     }
-                    ++nv;
-                    if (more) ++nk;
+                    st = st1;
+                    ph = ph1;
                 }
                 if (!ok) break;
                 if (ptx::elect_one_sync()) ptx::mma_commit(&o_full);
@@ -710,7 +713,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             }
             ptx::tc_fence_before();
             if (!whole) {
-                const int first = pc.first, n = pc.pieces;
+                auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
+                const int first = cta_of(u0 + pc.item0);
+                const int n = cta_of(u0 + pc.item0 + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
                 ptx::named_bar_sync(1, 256);
                 if (threadIdx.x == 256) {
                     __threadfence();
