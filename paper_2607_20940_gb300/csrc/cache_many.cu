@@ -15,8 +15,8 @@
 //   warp 2      the CTA's pieces, into a ring that the others read
 //   warp 3      codes and scales of a step's keys, then values, into a ring: a
 //               bulk copy per record of 16 tokens
-//   warps 4-7   codes to f16: code times scale, which f16 holds exactly, from the
-//               ring into 128-byte-swizzled tiles
+//   warps 4-7   codes to f16 (two warps the keys, two the values): code times scale,
+//               which f16 holds exactly, from the ring into 128-byte-swizzled tiles
 //   warps 8-11  softmax of tile 0, warps 12-15 of tile 1: a thread per row. They
 //               also put Q into shared memory, as f16 with the row's largest value
 //               near 2^14 (the row's power of two joins the softmax scale)
@@ -29,8 +29,6 @@
 // (9/8 D bytes a token) with few. Every wait is bounded.
 #include <cuda_runtime.h>
 #include <math.h>
-
-#include <type_traits>
 
 #include "cache.h"
 #include "cache_codes.cuh"
@@ -127,16 +125,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         abort_flag = 0;
         ptx::mbar_init(&q_full, 8);
         for (int s = 0; s < kK; ++s) {
-            ptx::mbar_init(&k_full[s], 4);
+            ptx::mbar_init(&k_full[s], 2);
             ptx::mbar_init(&k_empty[s], 1);
         }
         for (int s = 0; s < kV; ++s) {
-            ptx::mbar_init(&v_full[s], 4);
+            ptx::mbar_init(&v_full[s], 2);
             ptx::mbar_init(&v_empty[s], 1);
         }
         for (int s = 0; s < kMaxCodes; ++s) {
             ptx::mbar_init(&c_full[s], 1);
-            ptx::mbar_init(&c_empty[s], 4);
+            ptx::mbar_init(&c_empty[s], 2);
         }
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&s_full[t], 1);
@@ -429,67 +427,65 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     } else if (warp < 8) {
         ptx::setmaxnreg_dec<kCodeRegs>();
         // ============================ codes to f16 ============================
-        // A unit is 32 neighbouring dims of a token: 16 bytes of codes, two
-        // scales, 64 bytes of f16. A thread has the same token and dims of every
-        // kRecStep-th record. Eight lanes take four tokens and two chunks of 32
-        // dims, so that their 16-byte stores lie in eight different slots of the
-        // swizzled rows.
-        constexpr int kIt = D / 32, kPer = 16 * (D / 32);  // a thread's units of a step; units of a record
-        constexpr int kRecStep = 128 / kPer;               // records that the threads take at a time
-        const int x = (int)threadIdx.x - 128;
+        // Warps 4 and 5 have the keys, 6 and 7 the values. A unit is 32 neighbouring
+        // dims of a token: 16 bytes of codes, two scales, 64 bytes of f16. A thread
+        // has the same token and dims of every kRecStep-th record. Eight lanes take
+        // four tokens and two chunks of 32 dims, so that their 16-byte stores lie in
+        // eight different slots of the swizzled rows.
+        constexpr int kPer = 16 * (D / 32);   // units of a record
+        constexpr int kRecStep = 64 / kPer;   // records that a pair of warps takes at a time
+        constexpr int kBatch = 4, kBatches = 8 / kRecStep / kBatch;
+        const bool values = warp >= 6;
+        const int x = (int)threadIdx.x % 64;
         const int chunk = (x & 1) + (D == 128 ? x >> 2 & 2 : 0);
         const int rest = (x >> 1 & 3) + (D == 128 ? x >> 4 << 2 : x >> 3 << 2);  // token among kRecStep records'
         const int tok = rest % 16, rec0 = rest / 16;
-        const uint32_t k_at = rec0 * cache_v_codes(D) + tok * (D / 2) + chunk * 16;
-        const uint32_t ks_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + tok * (D / 16) + chunk * 2;
-        const uint32_t v_at = rec0 * cache_v_codes(D) + tok * (D / 2) + cache_v_code_at(D, tok, chunk * 16);
-        const uint32_t vs_at = rec0 * cache_v_codes(D) + cache_k_scales(D) + chunk * 32 + cache_v_scale_at(tok);
+        const uint32_t codes_at = rec0 * cache_v_codes(D) + tok * (D / 2) + (values ? cache_v_code_at(D, tok, chunk * 16) : chunk * 16);
+        const uint32_t scales_at = rec0 * cache_v_codes(D) + cache_k_scales(D) +
+                                   (values ? chunk * 32 + cache_v_scale_at(tok) : tok * (D / 16) + chunk * 2);
+        const uint32_t second = values ? 16 : 1;  // from a unit's first scale to its second
         const int row0 = 16 * rec0 + tok;  // of the tile; the next is 16 kRecStep rows on
         const uint32_t tile_at = (uint32_t)((chunk >> 1) * (kTile * 128) + row0 * 128);
         const uint32_t slot = (uint32_t)(((chunk & 1) * 4) ^ (row0 & 7)) << 4;
-        int half = 0, n_tiles = 0, pieces = 0;
-        // Half a step: the codes in slot `half` of the ring to f16 in `tile`.
-        // left: tokens of the step that the sequence has (values past it: zeros).
-        auto convert = [&](unsigned char* tile, auto values, int left) {
-            constexpr bool kValues = decltype(values)::value;
-            const int sl = half % n_codes;
+        int n_tiles = 0, pieces = 0;
+        // Half of step n_tiles: its codes in the ring to f16 in `tile`. left: tokens
+        // of the step that the sequence has (values past it: zeros).
+        auto convert = [&](unsigned char* tile, int left) {
+            const int half = 2 * n_tiles + values, sl = half % n_codes;
             ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&c_full[sl], (uint32_t)(half / n_codes & 1), abort_p, wait_limit));
             if (!ok) return;
             const unsigned char* src = sC + sl * C::kCode;
-            uint4 w[kIt];
-            uint32_t sc[kIt];
-#pragma unroll
-            for (int i = 0; i < kIt; ++i) {
-                const unsigned char* rec = src + i * (kRecStep * cache_v_codes(D));
-                w[i] = *reinterpret_cast<const uint4*>(rec + (kValues ? v_at : k_at));
-                if constexpr (kValues)
-                    sc[i] = rec[vs_at] | (uint32_t)rec[vs_at + 16] << 8;
-                else
-                    sc[i] = *reinterpret_cast<const uint16_t*>(rec + ks_at);
-            }
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&c_empty[sl]);
-            ++half;
-            if (kValues && left < kTile) {
-#pragma unroll
-                for (int i = 0; i < kIt; ++i)
-                    if (row0 + 16 * kRecStep * i >= left) sc[i] = 0;
-            }
             unsigned char* to = tile + tile_at;
 #pragma unroll
-            for (int i = 0; i < kIt; ++i) {
-                const uint32_t two = codes::e4m3_f16x2(sc[i]);
-                const uint32_t s0 = __byte_perm(two, 0, 0x1010), s1 = __byte_perm(two, 0, 0x3232);
-                const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            for (int b = 0; b < kBatches; ++b) {
+                uint4 w[kBatch];
+                uint32_t sc[kBatch];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t sq = q < 2 ? s0 : s1;
-                    uint4 o;
-                    o.x = codes::mul_f16x2(codes::e2m1_f16x2<0>(cw[q]), sq);
-                    o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(cw[q]), sq);
-                    o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(cw[q]), sq);
-                    o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(cw[q]), sq);
-                    *reinterpret_cast<uint4*>(to + (slot ^ (uint32_t)(q << 4)) + i * (16 * kRecStep * 128)) = o;
+                for (int i = 0; i < kBatch; ++i) {
+                    const unsigned char* rec = src + (b * kBatch + i) * (kRecStep * cache_v_codes(D));
+                    w[i] = *reinterpret_cast<const uint4*>(rec + codes_at);
+                    sc[i] = rec[scales_at] | (uint32_t)rec[scales_at + second] << 8;
+                    if (values && row0 + 16 * kRecStep * (b * kBatch + i) >= left) sc[i] = 0;
+                }
+                if (b == kBatches - 1) {
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&c_empty[sl]);
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const uint32_t two = codes::e4m3_f16x2(sc[i]);
+                    const uint32_t s0 = __byte_perm(two, 0, 0x1010), s1 = __byte_perm(two, 0, 0x3232);
+                    const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t sq = q < 2 ? s0 : s1;
+                        uint4 o;
+                        o.x = codes::mul_f16x2(codes::e2m1_f16x2<0>(cw[q]), sq);
+                        o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(cw[q]), sq);
+                        o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(cw[q]), sq);
+                        o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(cw[q]), sq);
+                        *reinterpret_cast<uint4*>(to + (slot ^ (uint32_t)(q << 4)) + (b * kBatch + i) * (16 * kRecStep * 128)) = o;
+                    }
                 }
             }
         };
@@ -503,19 +499,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             if (lane == 0) ptx::mbar_arrive(bar);
         };
         static_assert(kK == kV, "one count of tiles");
+        unsigned char* const tiles = values ? sV : sK;
+        uint64_t *const bar_empty = values ? v_empty : k_empty, *const bar_full = values ? v_full : k_full;
         while (ok && piece(pieces, pc)) {
             for (int j = pc.b0; j < pc.b1; ++j, ++n_tiles) {
                 const int st = n_tiles % kK;
-                const uint32_t par = (uint32_t)(n_tiles / kK & 1);
-                const int left = pc.len - j * kTile;
-                if (!room(&k_empty[st], par)) break;
-                convert(sK + st * C::kBytes, std::false_type{}, left);
+                if (!room(&bar_empty[st], (uint32_t)(n_tiles / kK & 1))) break;
+                convert(tiles + st * C::kBytes, pc.len - j * kTile);
                 if (!ok) break;
-                give(&k_full[st]);
-                if (!room(&v_empty[st], par)) break;
-                convert(sV + st * C::kBytes, std::true_type{}, left);
-                if (!ok) break;
-                give(&v_full[st]);
+                give(&bar_full[st]);
             }
             done(pieces);
             ++pieces;
