@@ -77,6 +77,26 @@ __host__ __device__ inline int cache_need(const CacheView& c, int tokens) {
     return (int)(((long long)tokens + c.P - 1) >> c.log2_p);
 }
 
+// n / d for 0 <= n < 2^31 by a product with 2^(31 + l) / d, rounded up, where
+// 2^(l - 1) < d <= 2^l (Granlund and Montgomery, "Division by invariant integers
+// using multiplication", 1994).
+struct FastDiv {
+    int d;
+    uint32_t mul;
+    int shift;
+    explicit FastDiv(int by = 1) : d(by), mul(0), shift(0) {
+        int l = 0;
+        while ((1ll << l) < by) ++l;
+        if (by > 1) {
+            mul = (uint32_t)(((1ull << (31 + l)) + by - 1) / by);
+            shift = l - 1;
+        }
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift); }
+#endif
+};
+
 struct CacheAttnArgs {
     const uint16_t* q;
     uint16_t* out;
@@ -84,7 +104,8 @@ struct CacheAttnArgs {
     const uint16_t* base_out;
     const float* base_lse;
     long long q_st[3], o_st[3], l_st[2];
-    int queries, heads, group;  // group: heads / Hk
+    int queries, heads;
+    FastDiv group;  // heads / Hk
     int causal;
     int layer, n;
     const int* seqs;

@@ -238,7 +238,7 @@ static msf_status attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, 
     a.l_st[1] = x.lse_strides[1];
     a.queries = x.queries;
     a.heads = x.heads;
-    a.group = x.heads / cache->d.kv_heads;
+    a.group = msf::FastDiv(x.heads / cache->d.kv_heads);
     a.causal = x.causal;
     a.layer = layer;
     a.n = n;

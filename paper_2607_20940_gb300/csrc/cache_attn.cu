@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
     const int h = x % a.heads;
     x /= a.heads;
     const int t = x % a.queries, i = x / a.queries;
-    const int s = a.seqs ? a.seqs[i] : i, hk = h / a.group;
+    const int s = a.seqs ? a.seqs[i] : i, hk = a.group.div(h);
     int len = 0;
     if ((unsigned)s < (unsigned)c.S)
         len = min(c.lengths[s], c.W * c.P);
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     __shared__ int s_merge[2];
     __shared__ int abort_flag;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-    const int rows = a.group * a.queries;
+    const int rows = a.group.d * a.queries;
     unsigned char* ring = smem + warp * C::kOwn;
     auto part_of = [&](int w, int last) {  // the first piece of warp w, or its last
         return reinterpret_cast<float*>(last ? smem + w * C::kOwn : smem + kW * C::kOwn + w * C::kPart);
@@ -282,10 +282,12 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     auto units_of = [&](int len) { return len > 0 ? pairs_of(len) + kItem : 0; };
     // Row r of (row i of the list, key head hk): its place in q, out and lse.
     auto place = [&](const long long* st, int i, int hk, int r) {
-        return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
+        const int u = a.group.div(r);
+        return i * st[0] + u * st[1] + (hk * a.group.d + r - u * a.group.d) * st[2];
     };
     auto lse_place = [&](int i, int hk, int r) {
-        return i * a.l_st[0] + (hk * a.group + r % a.group) * a.l_st[1] + r / a.group;
+        const int u = a.group.div(r);
+        return i * a.l_st[0] + (hk * a.group.d + r - u * a.group.d) * a.l_st[1] + u;
     };
     // Sum of `x` over the block's threads before this one; all: over all.
     auto scan = [&](long long x, long long& all) {
@@ -447,7 +449,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             for (int x = 0; x < 2; ++x) {
                 f[nt][x] = codes::row_factor(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x)), a.scale * c.k_unit);
                 const int rr = 8 * nt + 2 * t + x;
-                limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + rr / a.group : len;
+                limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + a.group.div(rr) : len;
             }
         }
         // no token below this one is hidden from a row
@@ -835,7 +837,7 @@ cudaError_t launch_cache_attend_simt(const CacheView& c, const CacheAttnArgs& a,
 }
 
 cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
-    const long long rows = (long long)a.group * a.queries;
+    const long long rows = (long long)a.group.d * a.queries;
     if (rows <= 8) return c.D == 128 ? launch_few<128, 1>(c, a, st) : launch_few<64, 1>(c, a, st);
     if (rows <= 16) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
     return launch_cache_attend_many(c, a, st);

@@ -11,7 +11,7 @@
 // Roles (512 threads):
 //   warp 0      MMA issuer: S_t = Q_t K^T (both from shared memory), O_t += P_t V
 //               (P from TMEM), f16 in fp32
-//   warp 1      TMEM (all 512 columns)
+//   warp 1      TMEM (all 512 columns); rows of blocks that see no token
 //   warp 2      the CTA's pieces, into a ring that the others read
 //   warp 3      codes and scales of a step's keys, then values, into a ring: a
 //               bulk copy per record of 16 tokens
@@ -74,6 +74,7 @@ struct Piece {
     int item0;          // the item's first unit, from the CTA's first
 };
 constexpr int kPieces = 4;
+constexpr int kItem = 5;
 
 struct Shape {
     const CacheView& c;
@@ -81,7 +82,7 @@ struct Shape {
     int rows, blocks;
 
     __device__ Shape(const CacheView& c_, const CacheAttnArgs& a_)
-        : c(c_), a(a_), rows(a_.group * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
+        : c(c_), a(a_), rows(a_.group.d * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
     __device__ int length(int i) const {
         const int s = a.seqs ? a.seqs[i] : i;
         return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
@@ -89,14 +90,19 @@ struct Shape {
     __device__ int block_rows(int b) const { return min(kBlock, rows - b * kBlock); }
     __device__ int tiles(int b) const { return (block_rows(b) + kTile - 1) / kTile; }
     __device__ int steps(int n, int b) const {
-        if (a.causal) n = min(n, max(0, n - a.queries + 1 + (b * kBlock + block_rows(b) - 1) / a.group));
+        if (a.causal) n = min(n, max(0, n - a.queries + 1 + a.group.div(b * kBlock + block_rows(b) - 1)));
         return (n + kTile - 1) / kTile;
     }
-    // Units (steps of one tile) of a key head of a sequence of n tokens.
+    // Units of an item, and of a key head of a sequence of n tokens: a step of one
+    // tile, and kItem for what an item costs besides its steps.
+    __device__ int units(int n, int b) const {
+        const int k = steps(n, b);
+        return k > 0 ? kItem + k * tiles(b) : 0;
+    }
     __device__ long long head_units(int n) const {
-        if (!a.causal) return (long long)((n + kTile - 1) / kTile) * ((rows + kTile - 1) / kTile);
+        if (!a.causal) return n > 0 ? (long long)((n + kTile - 1) / kTile) * ((rows + kTile - 1) / kTile) + (long long)kItem * blocks : 0;
         long long u = 0;
-        for (int b = 0; b < blocks; ++b) u += (long long)steps(n, b) * tiles(b);
+        for (int b = 0; b < blocks; ++b) u += units(n, b);
         return u;
     }
 };
@@ -109,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     unsigned char* sK = smem;
     unsigned char* sV = sK + kK * C::kBytes;
     unsigned char* sQ = sV + kV * C::kBytes;
-    const bool one_tile = a.group * a.queries <= kTile;
+    const bool one_tile = a.group.d * a.queries <= kTile;
     unsigned char* sC = sQ + (one_tile ? 1 : 2) * C::kBytes;
     const int n_codes = one_tile ? C::kCodes1 : C::kCodes;
     __shared__ uint64_t c_full[kMaxCodes], c_empty[kMaxCodes], q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
@@ -119,6 +125,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __shared__ uint32_t tmem_base_sh;
     __shared__ int abort_flag, s_last;
     __shared__ long long s_scan[kThreads / 32], s_found[2];
+    __shared__ long long s_units[2];  // all units; this CTA's first
+    __shared__ int s_begin[3];  // the item that the share begins in: key head, block, its first unit from the share's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
@@ -162,31 +170,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 
     const Shape shape(c, a);
     auto place = [&](const long long* st, int i, int hk, int r) {
-        return i * st[0] + (r / a.group) * st[1] + (hk * a.group + r % a.group) * st[2];
+        const int t = a.group.div(r);
+        return i * st[0] + t * st[1] + (hk * a.group.d + r - t * a.group.d) * st[2];
     };
     auto lse_place = [&](int i, int hk, int r) {
-        return i * a.l_st[0] + (hk * a.group + r % a.group) * a.l_st[1] + r / a.group;
+        const int t = a.group.div(r);
+        return i * a.l_st[0] + (hk * a.group.d + r - t * a.group.d) * a.l_st[1] + t;
     };
-
-    // ---- blocks that see no token: their rows are empty, or the base's
-    for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * shape.blocks; x += gridDim.x) {
-        const int b = (int)(x % shape.blocks), hk = (int)(x / shape.blocks % c.Hk), i = (int)(x / shape.blocks / c.Hk);
-        if (shape.steps(shape.length(i), b) > 0) continue;
-        if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
-        const int n = shape.block_rows(b);
-        for (int y = threadIdx.x; y < n * (D / 8); y += kThreads) {
-            const int r = b * kBlock + y / (D / 8), d = y % (D / 8) * 8;
-            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
-                w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
-            *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
-        }
-        if (a.lse && a.lse != a.base_lse)
-            for (int y = threadIdx.x; y < n; y += kThreads) {
-                const long long at = lse_place(i, hk, b * kBlock + y);
-                a.lse[at] = a.base_lse ? a.base_lse[at] : -INFINITY;
-            }
-    }
 
     // ---- this CTA's share
     auto scan = [&](long long x, long long& all) {
@@ -208,13 +198,23 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         return before + v - x;
     };
     long long U = 0, mine = 0;
-    for (int i = threadIdx.x; i < a.n; i += kThreads) mine += shape.head_units(shape.length(i));
-    scan(mine, U);
+    bool none = false;  // whether a block sees no token
+    for (int i = threadIdx.x; i < a.n; i += kThreads) {
+        const int len = shape.length(i);
+        none |= shape.steps(len, 0) == 0;
+        mine += shape.head_units(len);
+    }
+    const long long before_mine = scan(mine, U) * c.Hk;
     U *= c.Hk;
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
     const bool idle = (int)blockIdx.x >= G || U == 0;
     const long long u0 = idle ? 0 : U * blockIdx.x / G, u1 = idle ? 0 : U * (blockIdx.x + 1) / G;
-    if (!idle) {
+    if (a.n <= kThreads) {
+        if (!idle && u0 >= before_mine && u0 < before_mine + mine * c.Hk) {
+            s_found[0] = threadIdx.x;
+            s_found[1] = before_mine;
+        }
+    } else if (!idle) {
         long long base = 0;
         for (int i0 = 0; i0 < a.n; i0 += kThreads) {
             const int i = i0 + (int)threadIdx.x;
@@ -227,6 +227,23 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             }
             base += all;
             if (u0 < base) break;
+        }
+    }
+    if (threadIdx.x == 0) {
+        s_units[0] = U;
+        s_units[1] = u0;
+    }
+    none = __syncthreads_or(none);
+    // The block that the share begins in, where a head's blocks are no more than the threads.
+    if (!idle && shape.blocks <= kThreads) {
+        const int len = shape.length((int)s_found[0]);
+        long long per;
+        const long long before = scan((int)threadIdx.x < shape.blocks ? shape.units(len, threadIdx.x) : 0, per);
+        const long long in = u0 - s_found[1], hk = in / per, rest = in - hk * per;
+        if ((int)threadIdx.x < shape.blocks && rest >= before && rest < before + shape.units(len, threadIdx.x)) {
+            s_begin[0] = (int)hk;
+            s_begin[1] = threadIdx.x;
+            s_begin[2] = (int)(before - rest);
         }
     }
     __syncthreads();
@@ -249,16 +266,19 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         if (warp == 2) {
             // ============================== pieces ==============================
             if (lane == 0) {
-                // All from this CTA's first unit. The head that the share begins in
-                // may begin before it.
+                // Units are counted from this CTA's first.
                 const int end = (int)(u1 - u0);
                 int seq = 0, hk = 0, blk = 0, len = 0, at = 0;
                 if (end > 0) {
                     seq = (int)s_found[0];
                     len = shape.length(seq);
-                    const long long per = shape.head_units(len);
-                    hk = (int)((u0 - s_found[1]) / per);
-                    at = (int)(s_found[1] + hk * per - u0);
+                    if (shape.blocks <= kThreads) {
+                        hk = s_begin[0], blk = s_begin[1], at = s_begin[2];
+                    } else {
+                        const long long per = shape.head_units(len);
+                        hk = (int)((u0 - s_found[1]) / per);
+                        at = (int)(s_found[1] + hk * per - u0);
+                    }
                 }
                 for (int n = 0;; ++n) {
                     if (!ptx::mbar_wait_bounded(&pc_empty[n % kPieces], (uint32_t)(n / kPieces & 1) ^ 1u, abort_p, wait_limit)) {
@@ -269,14 +289,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     p.steps = 0;
                     while (at < end && p.steps == 0) {
                         const int steps = shape.steps(len, blk), w = shape.tiles(blk);
-                        // step k belongs to the CTA that has unit at + k w
-                        const int b0 = at < 0 ? min(steps, (-at + w - 1) / w) : 0, b1 = min(steps, (end - at + w - 1) / w);
+                        // step k belongs to the CTA that has unit at + kItem + k w
+                        const int from = at + kItem;
+                        const int b0 = from < 0 ? min(steps, (-from + w - 1) / w) : 0;
+                        const int b1 = end > from ? min(steps, (end - from + w - 1) / w) : 0;
                         if (b0 < b1) {
                             p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
                             p.rows = shape.block_rows(blk), p.tiles = w, p.steps = steps;
                             p.b0 = b0, p.b1 = b1, p.item0 = at;
                         }
-                        at += steps * w;
+                        if (steps > 0) at += kItem + steps * w;
                         if (++blk == shape.blocks) {
                             blk = 0;
                             if (++hk == c.Hk) {
@@ -290,6 +312,26 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ptx::mbar_arrive(&pc_full[n % kPieces]);
                     if (!some) break;
                 }
+            }
+        } else if (warp == 1 && none) {
+            // ====== blocks that see no token: their rows are empty, or the base's ======
+            for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * shape.blocks; x += gridDim.x) {
+                const int b = (int)(x % shape.blocks), hk = (int)(x / shape.blocks % c.Hk), i = (int)(x / shape.blocks / c.Hk);
+                if (shape.steps(shape.length(i), b) > 0) continue;
+                if (lane == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
+                const int n = shape.block_rows(b);
+                for (int y = lane; y < n * (D / 8); y += 32) {
+                    const int r = b * kBlock + y / (D / 8), d = y % (D / 8) * 8;
+                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                    if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
+                        w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
+                    *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+                }
+                if (a.lse && a.lse != a.base_lse)
+                    for (int y = lane; y < n; y += 32) {
+                        const long long at = lse_place(i, hk, b * kBlock + y);
+                        a.lse[at] = a.base_lse ? a.base_lse[at] : -INFINITY;
+                    }
             }
         } else if (warp == 3) {
             // ============================== codes ==============================
@@ -546,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const int e2 = codes::row_exponent(top);
                 const float up = codes::row_up(e2);
                 f = codes::row_factor(e2, a.scale * c.k_unit);
-                limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + R / a.group : pc.len;
+                limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + a.group.div(R) : pc.len;
 #pragma unroll
                 for (int e = 0; e < D / 8; ++e) {
                     uint32_t y[4];
@@ -661,9 +703,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 jn = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
                 if (a.lse) a.lse[at] = jn.lse;
             };
-            auto store = [&](int d, const uint32_t (&o)[32]) {  // 32 dims of the row's result
+            auto store = [&](int d, const uint32_t (&o)[16]) {  // 16 dims of the row's result
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 2; ++e) {
                     float y[8];
 #pragma unroll
                     for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[8 * e + z]) * jn.own;
@@ -688,26 +730,31 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (whole && live) finish(m, l);
 #pragma unroll 1
                 for (int d = 0; d < D; d += 32) {
-                    uint32_t o[32];
-                    ptx::tmem_ld32(tO + d, o);
+                    uint32_t o[2][16];
+                    ptx::tmem_ld16(tO + d, o[0]);
+                    ptx::tmem_ld16(tO + d + 16, o[1]);
                     ptx::tmem_wait_ld();
-                    if (whole) {
-                        if (live) store(d, o);
-                    } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            __stcg(reinterpret_cast<float4*>(slot) + (d / 4 + e) * kBlock + sr,
-                                   make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                               __uint_as_float(o[4 * e + 3])));
+                    for (int h = 0; h < 2; ++h) {
+                        if (whole) {
+                            if (live) store(d + 16 * h, o[h]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                __stcg(reinterpret_cast<float4*>(slot) + (d / 4 + 4 * h + e) * kBlock + sr,
+                                       make_float4(__uint_as_float(o[h][4 * e]), __uint_as_float(o[h][4 * e + 1]),
+                                                   __uint_as_float(o[h][4 * e + 2]), __uint_as_float(o[h][4 * e + 3])));
+                        }
                     }
                 }
                 if (!whole) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
             }
             ptx::tc_fence_before();
             if (!whole) {
-                auto cta_of = [&](long long u) { return (int)(((u + 1) * G - 1) / U); };
-                const int first = cta_of(u0 + pc.item0);
-                const int n = cta_of(u0 + pc.item0 + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
+                const long long all = s_units[0], u = s_units[1] + pc.item0 + kItem;
+                const int ctas = (int)min((long long)gridDim.x, max(1ll, all / 2));
+                auto cta_of = [&](long long v) { return (int)(((v + 1) * ctas - 1) / all); };
+                const int first = cta_of(u), n = cta_of(u + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
                 ptx::named_bar_sync(1, 256);
                 if (threadIdx.x == 256) {
                     __threadfence();
@@ -728,22 +775,33 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     }
                     finish(M, L);
 #pragma unroll 1
-                    for (int d = 0; d < D; d += 32) {
-                        uint32_t o[32];
+                    for (int d = 0; d < D; d += 16) {
+                        uint32_t o[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                        for (int e = 0; e < 16; ++e) o[e] = 0u;
+                        // kTogether pieces' loads at a time: each round trip costs half a microsecond
+                        constexpr int kTogether = 4;
 #pragma unroll 1
-                        for (int k = 0; k < n; ++k) {
-                            const float w = codes::ex2(__ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr).x - M);
-                            float4 y[8];
+                        for (int k = 0; k < n; k += kTogether) {
+                            float4 y[kTogether][4];
+                            float w[kTogether];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(slot_of(k)) + (d / 4 + e) * kBlock + sr);
+                            for (int z = 0; z < kTogether; ++z) {
+                                const float* from = slot_of(min(k + z, n - 1));
+                                w[z] = __ldcg(reinterpret_cast<const float2*>(from + kBlock * D) + sr).x;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                o[4 * e] = __float_as_uint(fmaf(w, y[e].x, __uint_as_float(o[4 * e])));
-                                o[4 * e + 1] = __float_as_uint(fmaf(w, y[e].y, __uint_as_float(o[4 * e + 1])));
-                                o[4 * e + 2] = __float_as_uint(fmaf(w, y[e].z, __uint_as_float(o[4 * e + 2])));
-                                o[4 * e + 3] = __float_as_uint(fmaf(w, y[e].w, __uint_as_float(o[4 * e + 3])));
+                                for (int e = 0; e < 4; ++e) y[z][e] = __ldcg(reinterpret_cast<const float4*>(from) + (d / 4 + e) * kBlock + sr);
+                            }
+#pragma unroll
+                            for (int z = 0; z < kTogether; ++z) {
+                                const float f = k + z < n ? codes::ex2(w[z] - M) : 0.f;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    o[4 * e] = __float_as_uint(fmaf(f, y[z][e].x, __uint_as_float(o[4 * e])));
+                                    o[4 * e + 1] = __float_as_uint(fmaf(f, y[z][e].y, __uint_as_float(o[4 * e + 1])));
+                                    o[4 * e + 2] = __float_as_uint(fmaf(f, y[z][e].z, __uint_as_float(o[4 * e + 2])));
+                                    o[4 * e + 3] = __float_as_uint(fmaf(f, y[z][e].w, __uint_as_float(o[4 * e + 3])));
+                                }
                             }
                         }
                         store(d, o);
