@@ -34,7 +34,7 @@ __host__ __device__ constexpr int cache_v_scale_at(int token) {
 }
 
 // Words of the state's header.
-enum : int { kCacheStatus = 0, kCacheCopies = 1, kCacheBad = 2, kCacheLive = 3 };
+enum : int { kCacheStatus = 0, kCacheCopies = 1, kCacheLive = 2 };
 // Bits of the status word beside kDevTimeout.
 constexpr unsigned kDevPages = 2u, kDevIndex = 4u, kDevNonfinite = 8u;
 constexpr unsigned kCacheStop = kDevPages | kDevIndex;  // nothing changes the cache until these are read

@@ -77,13 +77,24 @@ __device__ bool find_free(const CacheView& c, int want, int* sh) {
     return found >= want;
 }
 
+// Lanes of a warp that call together are often at neighbouring pages: one atomic a word.
+__device__ __forceinline__ void set_used(const CacheView& c, int page, bool on) {
+    const unsigned lanes = __match_any_sync(__activemask(), page / 32);
+    const unsigned bits = __reduce_or_sync(lanes, 1u << page % 32);
+    if (__ffs(lanes) - 1 == (int)(threadIdx.x % 32)) {
+        if (on)
+            atomicOr(c.used + page / 32, bits);
+        else
+            atomicAnd(c.used + page / 32, ~bits);
+    }
+}
 __device__ __forceinline__ void take_page(const CacheView& c, int page) {
     c.refs[page] = 1;
-    atomicOr(c.used + page / 32, 1u << page % 32);
+    set_used(c, page, true);
 }
 __device__ __forceinline__ void drop_page(const CacheView& c, int page) {
     if (!cache_page_ok(c, page)) return;
-    if (atomicSub(c.refs + page, 1) == 1) atomicAnd(c.used + page / 32, ~(1u << page % 32));
+    if (atomicSub(c.refs + page, 1) == 1) set_used(c, page, false);
 }
 
 // ------------------------------------------------------------------- growing
@@ -136,21 +147,20 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
         if (want <= c.pages) want += total;
     }
     // (barriers: the rows' places and the claims are in place)
-    int err = __syncthreads_or((int)(bad & kDevIndex)) ? (int)kDevIndex : 0;
-    if (__syncthreads_or((int)(bad & kDevPages))) err |= (int)kDevPages;
-    if (!err && !find_free(c, (int)want, sh)) err = (int)kDevPages;
-    if (err) {
-        if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, (unsigned)err);
+    if (bad) atomicOr(c.head + kCacheStatus, bad);
+    if (__syncthreads_or((int)bad)) return;
+    if (!find_free(c, (int)want, sh)) {
+        if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevPages);
         return;
     }
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int i = warp; i < n; i += kThreads / 32) {
+    // A thread takes a row of a page or two, a warp a longer one.
+    auto give = [&](int i, int lane, int lanes, int most, int least) {
         const int s = seq_of(seqs, i), count = counts ? counts[i] : tokens, len = c.lengths[s];
-        if (count == 0) continue;
         const int copied = c.row[i] & 1, first = c.row[i] >> 1;
         const int col0 = copied ? len / c.P : cache_need(c, len);
-        const int k = cache_need(c, len + count) - col0;
-        for (int j = lane; j < k; j += 32) {
+        const int k = count > 0 ? cache_need(c, len + count) - col0 : 0;
+        if (k < least || k > most) return;
+        for (int j = lane; j < k; j += lanes) {
             const int page = c.free_list[first + j];
             int* entry = c.table + (size_t)s * c.W + col0 + j;
             if (copied && j == 0) {
@@ -160,9 +170,11 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
             *entry = page;
             take_page(c, page);
         }
-        __syncwarp();
-        if (lane == 0) c.lengths[s] = len + count;
-    }
+    };
+    for (int i = threadIdx.x; i < n; i += kThreads) give(i, 0, 1, 2, 1);
+    for (int i = threadIdx.x / 32; i < n; i += kThreads / 32) give(i, threadIdx.x % 32, 32, 0x7fffffff, 3);
+    __syncthreads();  // lengths are read until here
+    for (int i = threadIdx.x; i < n; i += kThreads) c.lengths[seq_of(seqs, i)] += counts ? counts[i] : tokens;
     __syncthreads();
     if (threadIdx.x == 0) c.head[kCacheCopies] = (unsigned)n_copies;
 }
@@ -191,15 +203,9 @@ __device__ bool list_check(const CacheView& c, const int* src, const int* dst, c
         else
             c.new_len[i] = min(__ldcg(c.lengths + s), keep);
     }
-    if (bad) atomicOr(c.head + kCacheBad, 1u);
+    if (bad) atomicOr(c.head + kCacheStatus, kDevIndex);
     ptx::cluster_sync();
-    const bool ok = __ldcg(c.head + kCacheBad) == 0;
-    ptx::cluster_sync();
-    if (!ok && t == 0) {
-        c.head[kCacheBad] = 0;
-        atomicOr(c.head + kCacheStatus, kDevIndex);
-    }
-    return ok;
+    return !(__ldcg(c.head + kCacheStatus) & kCacheStop);  // raised by this call: it was clear before
 }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
@@ -222,53 +228,45 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
                 if (want > c.pages) break;
             }
             if (want > c.pages || !find_free(c, (int)want, sh)) {
-                if (threadIdx.x == 0) {
-                    c.head[kCacheBad] = 1;
-                    atomicOr(c.head + kCacheStatus, kDevPages);
-                }
+                if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevPages);
             } else if (threadIdx.x == 0) {
                 c.head[kCacheCopies] = (unsigned)want;
             }
         }
         ptx::cluster_sync();
-        const bool ok = __ldcg(c.head + kCacheBad) == 0;
-        ptx::cluster_sync();
-        if (!ok) {
-            if (t == 0) c.head[kCacheBad] = 0;
-            return;
-        }
+        if (__ldcg(c.head + kCacheStatus) & kCacheStop) return;
     }
-    // The new rows, before any table changes.
-    const int warp = t / 32, lane = t % 32, warps = T / 32;
-    for (int i = warp; i < n; i += warps) {
-        const int* from = c.table + (size_t)src[i] * c.W;
-        int* to = c.stage + (size_t)i * c.W;
-        const int k = min(cache_need(c, __ldcg(c.new_len + i)), c.W), first = copy ? __ldcg(c.row + i) : 0;
-        for (int j = lane; j < k; j += 32) {
-            int page = __ldcg(from + j);
-            if (copy) {
-                const int own = __ldcg(c.free_list + first + j);
-                c.copies[first + j] = make_int2(page, own);
-                take_page(c, own);
-                page = own;
-            } else if (cache_page_ok(c, page)) {
-                atomicAdd(c.refs + page, 1);
-            }
-            to[j] = page;
+    // The new rows, before any table changes. A warp takes 32 columns of a row at a time.
+    const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
+    for (long long x = warp; x < (long long)n * strips; x += warps) {
+        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
+        if (j >= min(cache_need(c, __ldcg(c.new_len + i)), c.W)) continue;
+        int page = __ldcg(c.table + (size_t)src[i] * c.W + j);
+        if (copy) {
+            const int at = __ldcg(c.row + i) + j, own = __ldcg(c.free_list + at);
+            c.copies[at] = make_int2(page, own);
+            take_page(c, own);
+            page = own;
+        } else if (cache_page_ok(c, page)) {
+            atomicAdd(c.refs + page, 1);
         }
+        c.stage[(size_t)i * c.W + j] = page;
     }
     ptx::cluster_sync();
-    for (int i = warp; i < n; i += warps) {
-        const int d = dst[i], len = __ldcg(c.new_len + i);
-        const int* from = c.stage + (size_t)i * c.W;
-        int* to = c.table + (size_t)d * c.W;
-        const int k = min(cache_need(c, len), c.W), old = min(cache_need(c, __ldcg(c.lengths + d)), c.W);
-        for (int j = lane; j < max(k, old); j += 32) {
-            if (j < old) drop_page(c, __ldcg(to + j));
-            to[j] = j < k ? __ldcg(from + j) : -1;
+    for (long long x = warp; x < (long long)n * strips; x += warps) {
+        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
+        const int d = dst[i];
+        int* to = c.table + (size_t)d * c.W + j;
+        const int k = min(cache_need(c, __ldcg(c.new_len + i)), c.W);
+        if (j < c.W) {
+            const int old = __ldcg(to);  // -1 past the sequence's last page
+            if (old >= 0) drop_page(c, old);
+            if (j < k)
+                *to = __ldcg(c.stage + (size_t)i * c.W + j);
+            else if (old >= 0)
+                *to = -1;
         }
-        __syncwarp();
-        if (lane == 0) c.lengths[d] = len;
+        if (j == 0) c.lengths[d] = __ldcg(c.new_len + i);
     }
 }
 
@@ -278,17 +276,16 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     ptx::grid_dep_launch();
     const int t = (int)blockIdx.x * kThreads + (int)threadIdx.x, T = kCluster * kThreads;
     if (!list_check(c, nullptr, seqs, lengths, 0, n, t, T)) return;
-    const int warp = t / 32, lane = t % 32;
-    for (int i = warp; i < n; i += T / 32) {
+    const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
+    for (long long x = warp; x < (long long)n * strips; x += warps) {
+        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
         const int s = seq_of(seqs, i), len = __ldcg(c.new_len + i);
-        int* row = c.table + (size_t)s * c.W;
-        const int old = min(cache_need(c, __ldcg(c.lengths + s)), c.W);
-        for (int j = cache_need(c, len) + lane; j < old; j += 32) {
-            drop_page(c, row[j]);
-            row[j] = -1;
+        int* entry = c.table + (size_t)s * c.W + j;
+        if (j < c.W && j >= cache_need(c, len) && *entry >= 0) {
+            drop_page(c, *entry);
+            *entry = -1;
         }
-        __syncwarp();
-        if (lane == 0) c.lengths[s] = len;
+        if (j == 0) c.lengths[s] = len;
     }
 }
 
@@ -327,11 +324,22 @@ __global__ void __launch_bounds__(kThreads) cache_compact_kernel(const CacheView
     }
     __syncthreads();
     // holes == high: as many pages are missing below u as there are above it
-    for (int i = threadIdx.x; i < high; i += kThreads) {
-        const int2 p = c.copies[i];
-        c.moved[p.x] = p.y;
-        c.refs[p.y] = c.refs[p.x];
-        c.refs[p.x] = 0;
+    for (int i0 = threadIdx.x; i0 < high; i0 += 4 * kThreads) {
+        int2 p[4];
+        int r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i0 + e * kThreads < high) p[e] = c.copies[i0 + e * kThreads];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i0 + e * kThreads < high) r[e] = c.refs[p[e].x];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i0 + e * kThreads < high) {
+                c.moved[p[e].x] = p[e].y;
+                c.refs[p[e].y] = r[e];
+                c.refs[p[e].x] = 0;
+            }
     }
     for (int w = threadIdx.x; w < words; w += kThreads) {
         const int below = min(32, max(0, live - 32 * w));
@@ -345,55 +353,100 @@ __global__ void __launch_bounds__(kThreads) cache_compact_kernel(const CacheView
 
 // ------------------------------------------------------------------- copying
 
-// The pages of c.copies, all layers, 16 KB at a time; `follow`: and the tables
-// of a compaction.
-__global__ void __launch_bounds__(256) cache_copy_kernel(const CacheView c, int follow) {
-    constexpr int kVec = 4, kSeg = 256 * kVec;
+// The pages of c.copies, all layers: one warp of a CTA per SM moves them
+// through a ring of bulk copies into and out of shared memory, kAhead chunks
+// on their way in and as many out. `follow`: the other warps bring the tables
+// of a compaction in line.
+constexpr int kChunk = 18432, kSlots = 12, kAhead = 6;  // bytes at most, chunks in shared memory
+constexpr int kCopyThreads = 256;
+constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
+
+__global__ void __launch_bounds__(kCopyThreads) cache_copy_kernel(const CacheView c, int follow, int chunk, int chunks, long long wait_limit) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t full[kSlots];
+    __shared__ const uint8_t* s_from[64];
+    __shared__ uint8_t* s_to[64];
+    __shared__ uint32_t s_bytes[64];
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < kSlots; ++s) ptx::mbar_init(&full[s], 1);
+        ptx::fence_mbar_init();
+    }
+    __syncthreads();
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    const int n = (int)__ldcg(c.head + kCacheCopies);
-    const long long vecs = c.page_bytes / 16;
-    const int segs = (int)((vecs + kSeg - 1) / kSeg);
-    const long long items = (long long)n * c.L * segs;
-    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const int seg = (int)(it % segs);
-        const long long pl = it / segs;
-        const int layer = (int)(pl % c.L);
-        const int2 p = c.copies[pl / c.L];
-        if (!cache_page_ok(c, p.x) || !cache_page_ok(c, p.y)) continue;
-        const uint4* from = (const uint4*)(c.pool + ((long long)layer * c.pages + p.x) * c.page_bytes);
-        uint4* to = (uint4*)(c.pool + ((long long)layer * c.pages + p.y) * c.page_bytes);
-        uint4 x[kVec];
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-            const long long at = (long long)seg * kSeg + k * 256 + threadIdx.x;
-            if (at < vecs) x[k] = from[at];
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        const long long items = (long long)__ldcg(c.head + kCacheCopies) * c.L * chunks;
+        const int n = (int)blockIdx.x < items ? (int)((items - blockIdx.x + gridDim.x - 1) / gridDim.x) : 0;
+        bool ok = true;
+        int asked = 0, done = 0;
+        for (int b = 0; b < n + kAhead && ok; b += 32) {
+            // 32 chunks' places at a time
+            if (b + lane < n) {
+                const long long it = blockIdx.x + (long long)(b + lane) * gridDim.x, pl = it / chunks;
+                const int at = (int)(it - pl * chunks) * chunk;
+                const int2 p = c.copies[pl / c.L];
+                const long long layer = (pl % c.L) * c.pages;
+                const bool good = cache_page_ok(c, p.x) && cache_page_ok(c, p.y);
+                s_from[(b + lane) % 64] = c.pool + (layer + p.x) * c.page_bytes + at;
+                s_to[(b + lane) % 64] = c.pool + (layer + p.y) * c.page_bytes + at;
+                s_bytes[(b + lane) % 64] = good ? (uint32_t)min((long long)chunk, c.page_bytes - at) : 0u;
+            }
+            __syncwarp();
+            for (int i = b; i < min(b + 32, n + kAhead) && lane == 0; ++i) {
+                if (i < n) {
+                    // the copy out of the slot's last chunk has read it
+                    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kSlots - kAhead - 1) : "memory");
+                    const uint32_t bytes = s_bytes[i % 64];
+                    ptx::mbar_arrive_expect_tx(&full[i % kSlots], bytes);
+                    if (bytes > 0) ptx::bulk_load(smem + (i % kSlots) * kChunk, s_from[i % 64], bytes, &full[i % kSlots]);
+                    ++asked;
+                }
+                const int j = i - kAhead;
+                if (j >= 0) {
+                    ok = ptx::mbar_wait_bounded(&full[j % kSlots], (uint32_t)(j / kSlots & 1), &abort_flag, wait_limit);
+                    if (!ok) break;
+                    if (s_bytes[j % 64] > 0) ptx::bulk_store(s_to[j % 64], smem + (j % kSlots) * kChunk, s_bytes[j % 64]);
+                    ptx::bulk_commit();
+                    ++done;
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
         }
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-            const long long at = (long long)seg * kSeg + k * 256 + threadIdx.x;
-            if (at < vecs) to[at] = x[k];
+        if (lane == 0) {
+            if (!ok) {
+                atomicOr(c.head + kCacheStatus, kDevTimeout);
+                volatile int never = 0;
+                for (int i = done; i < asked; ++i)
+                    ptx::mbar_wait_bounded(&full[i % kSlots], (uint32_t)(i / kSlots & 1), &never, wait_limit);
+            }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     }
-    if (!follow) return;
+    if (!follow || threadIdx.x < 32) return;
     const int live = (int)__ldcg(c.head + kCacheLive);
     if (live == 0x7fffffff) return;
-    const int warp = (int)(blockIdx.x * blockDim.x + threadIdx.x) / 32, warps = (int)(gridDim.x * blockDim.x) / 32;
-    for (int s = warp; s < c.S; s += warps) {
-        int* row = c.table + (size_t)s * c.W;
-        const int k = min(cache_need(c, c.lengths[s]), c.W);
-        for (int j = threadIdx.x % 32; j < k; j += 32) {
-            const int page = row[j];
-            if (page >= live && page < c.pages) row[j] = c.moved[page];
-        }
+    const int per = kCopyThreads / 32 - 1, warps = (int)gridDim.x * per, strips = (c.W + 31) / 32;
+    for (long long x = (long long)blockIdx.x * per + threadIdx.x / 32 - 1; x < (long long)c.S * strips; x += warps) {
+        const int s = (int)(x / strips), j = 32 * (int)(x - (long long)s * strips) + (int)threadIdx.x % 32;
+        if (j >= c.W) continue;
+        int* entry = c.table + (size_t)s * c.W + j;
+        const int page = *entry;
+        if (page >= live && page < c.pages) *entry = c.moved[page];
     }
 }
 
 cudaError_t launch_copies(const CacheView& c, int follow, cudaStream_t st) {
     int sms;
-    const cudaError_t e = device_sms(&sms);
+    cudaError_t e = device_sms(&sms);
+    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_copy_kernel, kSlots * kChunk);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_copy_kernel, dim3(sms * 8), dim3(256), 0, st, c, follow);
+    // a page in equal chunks, multiples of 16 bytes
+    const int chunks = (int)((c.page_bytes + kChunk - 1) / kChunk);
+    const int chunk = (int)((c.page_bytes / 16 + chunks - 1) / chunks) * 16;
+    return launch_pdl(cache_copy_kernel, dim3(sms), dim3(kCopyThreads), kSlots * kChunk, st, c, follow, chunk, chunks, kWaitLimit);
 }
 
 }  // namespace

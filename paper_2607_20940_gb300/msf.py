@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -125,7 +126,6 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: run __graft_entry__.build() first")
     lib = ctypes.CDLL(LIB_PATH)
     P, VP, I32, SZ = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
-    I64P = ctypes.POINTER(ctypes.c_int64)
     sig = {
         "msf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "msf_last_cuda_error": (ctypes.c_int, []),
@@ -163,13 +163,13 @@ def _load():
         "msf_cache_query": (ctypes.c_int, [P, ctypes.POINTER(msf_cache_info)]),
         "msf_cache_bind": (ctypes.c_int, [P, VP, SZ, VP, SZ, VP, SZ]),
         "msf_cache_grow": (ctypes.c_int, [P, VP, VP, I32, I32, VP]),
-        "msf_cache_write": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, I64P, VP]),
-        "msf_cache_read": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, I64P, VP]),
+        "msf_cache_write": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, VP, VP]),
+        "msf_cache_read": (ctypes.c_int, [P, I32, VP, VP, I32, I32, VP, VP, VP, VP]),
         "msf_cache_fork": (ctypes.c_int, [P, VP, VP, VP, I32, I32, VP]),
         "msf_cache_truncate": (ctypes.c_int, [P, VP, VP, I32, VP]),
         "msf_cache_compact": (ctypes.c_int, [P, VP]),
-        "msf_cache_attend": (ctypes.c_int, [P, I32, VP, I32, ctypes.POINTER(msf_cache_attention), VP]),
-        "msf_cache_attend_simt": (ctypes.c_int, [P, I32, VP, I32, ctypes.POINTER(msf_cache_attention), VP]),
+        "msf_cache_attend": (ctypes.c_int, [P, I32, VP, I32, VP, VP]),
+        "msf_cache_attend_simt": (ctypes.c_int, [P, I32, VP, I32, VP, VP]),
         "msf_cache_device_status": (ctypes.c_int, [P, VP]),
     }
     for name, (res, args) in sig.items():
@@ -397,30 +397,50 @@ def msf_kernel_launches() -> int:
 
 
 # The cache (msf_cache.h). Tensors of rows are torch tensors, whose strides are
-# passed on; lists are int32 device tensors.
+# passed on; lists are int32 device tensors. A token's append or attention is a
+# few microseconds of device time, so these calls pack their C structures with
+# `struct` (a ctypes structure takes 0.2 us a field) and look torch up once.
+
+_torch = None
+
+
+def _get_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
 
 def _list(t, n=None):
     """An int32 device list (or None) and its length."""
     if t is None:
         return None, n
-    import torch
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype != _get_torch().int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("a list is a contiguous one-dimensional int32 tensor on the device")
-    if n is not None and t.numel() != n:
-        raise ValueError(f"a list has {t.numel()} entries where {n} are wanted")
-    return t.data_ptr(), t.numel()
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"a list has {t.shape[0]} entries where {n} are wanted")
+    return t.data_ptr(), t.shape[0]
 
 
 def _rows(t, dtype, name, shape=None):
     """Strides (elements) of a tensor of rows whose last dimension is contiguous."""
+    got = t.shape
     if t.dtype != dtype or not t.is_cuda:
         raise ValueError(f"{name}: a {dtype} tensor on the device is wanted")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, where {tuple(shape)} is wanted")
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if shape is not None and got != shape:
+        raise ValueError(f"{name}: shape {tuple(got)}, where {tuple(shape)} is wanted")
+    strides = t.stride()
+    if strides[-1] != 1 and got[-1] > 1 and t.numel():
         raise ValueError(f"{name}: the last dimension has to be contiguous")
-    # the stride of a dimension of one is anything
-    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+    if 1 in got:  # the stride of a dimension of one is anything
+        return tuple(x if n > 1 else 0 for x, n in zip(strides[:-1], got))
+    return strides[:-1]
+
+
+_STRIDES = struct.Struct("@3q")
+_ATTENTION = struct.Struct("@5P3q3q2q3if")
+assert _ATTENTION.size == ctypes.sizeof(msf_cache_attention)
 
 
 def msf_cache_create(desc: msf_cache_desc) -> int:
@@ -450,15 +470,16 @@ def msf_cache_grow(cache: int, seqs, counts, tokens: int, n: int, stream=None) -
 
 
 def _row_call(fn, where, cache, layer, k, v, seqs, at, stream):
-    import torch
-    if k.dim() != 4:
+    bf16 = _get_torch().bfloat16
+    shape = k.shape
+    if len(shape) != 4:
         raise ValueError(f"{where}: k and v are [rows, tokens, kv_heads, head_dim]")
-    strides = _rows(k, torch.bfloat16, "k")
-    if _rows(v, torch.bfloat16, "v", k.shape) != strides:
+    strides = _rows(k, bf16, "k")
+    if _rows(v, bf16, "v", shape) != strides:
         raise ValueError(f"{where}: k and v have the same strides")
-    n = k.shape[0]
-    _check(fn(cache, layer, _list(seqs, n)[0], _list(at, n)[0], n, k.shape[1], _ptr(k), _ptr(v),
-              (ctypes.c_int64 * 3)(*strides), _stream(stream)), where)
+    n = shape[0]
+    _check(fn(cache, layer, _list(seqs, n)[0], _list(at, n)[0], n, shape[1], k.data_ptr(), v.data_ptr(),
+              _STRIDES.pack(*strides), _stream(stream)), where)
 
 
 def msf_cache_write(cache: int, layer: int, k, v, seqs=None, counts=None, stream=None) -> None:
@@ -483,13 +504,13 @@ def msf_cache_compact(cache: int, stream=None) -> None:
     _check(_lib.msf_cache_compact(cache, _stream(stream)), "msf_cache_compact")
 
 
-def msf_cache_attend(cache: int, layer: int, seqs, n: int, args: msf_cache_attention, stream=None) -> None:
-    _check(_lib.msf_cache_attend(cache, layer, seqs, n, ctypes.byref(args), _stream(stream)), "msf_cache_attend")
+def msf_cache_attend(cache: int, layer: int, seqs, n: int, args: bytes, stream=None) -> None:
+    """args: the bytes of an msf_cache_attention."""
+    _check(_lib.msf_cache_attend(cache, layer, seqs, n, args, _stream(stream)), "msf_cache_attend")
 
 
-def msf_cache_attend_simt(cache: int, layer: int, seqs, n: int, args: msf_cache_attention, stream=None) -> None:
-    _check(_lib.msf_cache_attend_simt(cache, layer, seqs, n, ctypes.byref(args), _stream(stream)),
-           "msf_cache_attend_simt")
+def msf_cache_attend_simt(cache: int, layer: int, seqs, n: int, args: bytes, stream=None) -> None:
+    _check(_lib.msf_cache_attend_simt(cache, layer, seqs, n, args, _stream(stream)), "msf_cache_attend_simt")
 
 
 def msf_cache_device_status(cache: int, stream=None) -> int:
@@ -633,9 +654,11 @@ class Cache:
 
     def __init__(self, desc: msf_cache_desc):
         self.desc = desc
+        self.kv_heads, self.head_dim = desc.kv_heads, desc.head_dim
         self.handle = msf_cache_create(desc)
         self.info = msf_cache_query(self.handle)
         self.bound_pool = self.bound_state = self.bound_workspace = None
+        self.lengths = self.table = self.refs = None
 
     def close(self):
         if self.handle:
@@ -662,53 +685,34 @@ class Cache:
         return self._buffer(self.info.workspace_bytes, device)
 
     def bind(self, pool, state, workspace):
+        """Attach the buffers; the cache is empty then. `lengths` (tokens of each sequence), `table` (its
+        pages, -1 past the last) and `refs` (tables that name each page) are views of the state."""
         msf_cache_bind(self.handle, pool, state, workspace)
         self.bound_pool, self.bound_state, self.bound_workspace = pool, state, workspace
-
-    def _ints(self, offset, n):
-        import torch
-        return self.bound_state[int(offset):int(offset) + 4 * n].view(torch.int32)
-
-    @property
-    def lengths(self):
-        """Tokens of each sequence: a view of the state."""
-        return self._ints(self.info.lengths_offset, self.desc.sequences)
-
-    @property
-    def table(self):
-        """Pages of each sequence, -1 past its last: a view of the state."""
-        d = self.desc
-        return self._ints(self.info.table_offset, d.sequences * d.sequence_pages).view(d.sequences, d.sequence_pages)
-
-    @property
-    def refs(self):
-        """Tables that name each page, 0 for a free one: a view of the state."""
-        return self._ints(self.info.refs_offset, self.desc.pages)
+        d, i = self.desc, self.info
+        ints = lambda at, n: state[int(at):int(at) + 4 * n].view(_get_torch().int32)  # noqa: E731
+        self.lengths = ints(i.lengths_offset, d.sequences)
+        self.table = ints(i.table_offset, d.sequences * d.sequence_pages).view(d.sequences, d.sequence_pages)
+        self.refs = ints(i.refs_offset, d.pages)
 
     def grow(self, seqs=None, counts=None, tokens=0, stream=None):
         """Room for counts[i] (or `tokens`) more tokens of each listed sequence."""
-        n = self.desc.sequences
-        if seqs is not None:
-            n = seqs.numel()
-        elif counts is not None:
-            n = counts.numel()
+        n = seqs.shape[0] if seqs is not None else counts.shape[0] if counts is not None else self.desc.sequences
         msf_cache_grow(self.handle, _list(seqs, n)[0], _list(counts, n)[0], tokens, n, stream)
 
     def write(self, layer, k, v, seqs=None, counts=None, stream=None):
         """Quantise the newest tokens: k, v bf16 [rows, tokens, kv_heads, head_dim]."""
-        self._heads(k, v)
+        self._heads(k)
         msf_cache_write(self.handle, layer, k, v, seqs, counts, stream)
 
     def read(self, layer, k, v, seqs=None, begins=None, stream=None):
         """Read tokens from begins[i] on (0) back into bf16 k, v."""
-        self._heads(k, v)
+        self._heads(k)
         msf_cache_read(self.handle, layer, k, v, seqs, begins, stream)
 
-    def _heads(self, *rows):
-        for t in rows:
-            if tuple(t.shape[-2:]) != (self.desc.kv_heads, self.desc.head_dim):
-                raise ValueError(f"rows of {tuple(t.shape[-2:])} heads, where the cache holds "
-                                 f"{(self.desc.kv_heads, self.desc.head_dim)}")
+    def _heads(self, k):
+        if k.shape[-2:] != (self.kv_heads, self.head_dim):
+            raise ValueError(f"rows of {tuple(k.shape[-2:])} heads, where the cache holds {(self.kv_heads, self.head_dim)}")
 
     def fork(self, src, dst, lengths=None, copy=False, stream=None):
         """dst[i] becomes (the first lengths[i] tokens of) src[i], sharing its pages or with copies of them."""
@@ -716,11 +720,7 @@ class Cache:
 
     def truncate(self, seqs=None, lengths=None, stream=None):
         """Keep the first lengths[i] tokens (none) of each listed sequence."""
-        n = self.desc.sequences
-        if seqs is not None:
-            n = seqs.numel()
-        elif lengths is not None:
-            n = lengths.numel()
+        n = seqs.shape[0] if seqs is not None else lengths.shape[0] if lengths is not None else self.desc.sequences
         msf_cache_truncate(self.handle, _list(seqs, n)[0], _list(lengths, n)[0], n, stream)
 
     def compact(self, stream=None):
@@ -731,25 +731,29 @@ class Cache:
                softmax_scale=0.0, stream=None, simt=False):
         """Attention of q [rows, queries, heads, head_dim] over the listed sequences, joined with
         (base_out, base_lse) where given; lse [rows, heads, queries]. simt: on fp32 CUDA cores."""
-        import torch
-        if q.dim() != 4 or q.shape[3] != self.desc.head_dim:
-            raise ValueError(f"q is [rows, queries, heads, {self.desc.head_dim}]")
-        a = msf_cache_attention()
-        a.q, a.out, a.lse, a.base_out, a.base_lse = _ptr(q), _ptr(out), _ptr(lse), _ptr(base_out), _ptr(base_lse)
-        a.q_strides[:] = _rows(q, torch.bfloat16, "q")
-        a.out_strides[:] = _rows(out, torch.bfloat16, "out", q.shape)
-        if base_out is not None and _rows(base_out, torch.bfloat16, "base_out", q.shape) != list(a.out_strides):
+        torch = _torch or _get_torch()
+        shape = q.shape
+        if len(shape) != 4 or shape[3] != self.head_dim:
+            raise ValueError(f"q is [rows, queries, heads, {self.head_dim}]")
+        n, queries, heads, _ = shape
+        bf16 = torch.bfloat16
+        q_strides, strides = _rows(q, bf16, "q"), _rows(out, bf16, "out", shape)
+        if base_out is not None and base_out is not out and _rows(base_out, bf16, "base_out", shape) != strides:
             raise ValueError("base_out and out have the same strides")
-        n, queries, heads, _ = q.shape
-        for t, name in ((lse, "lse"), (base_lse, "base_lse")):
-            if t is not None:
-                strides = _rows(t, torch.float32, name, (n, heads, queries))
-                if name == "base_lse" and lse is not None and strides != list(a.lse_strides):
-                    raise ValueError("base_lse and lse have the same strides")
-                a.lse_strides[:] = strides
-        a.queries, a.heads, a.causal, a.softmax_scale = queries, heads, int(causal), softmax_scale
+        lse_strides = (0, 0)
+        if lse is not None:
+            lse_strides = _rows(lse, torch.float32, "lse", (n, heads, queries))
+        if base_lse is not None and base_lse is not lse:
+            base_strides = _rows(base_lse, torch.float32, "base_lse", (n, heads, queries))
+            if lse is not None and base_strides != lse_strides:
+                raise ValueError("base_lse and lse have the same strides")
+            lse_strides = base_strides
+        args = _ATTENTION.pack(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                               0 if base_out is None else base_out.data_ptr(),
+                               0 if base_lse is None else base_lse.data_ptr(), *q_strides, *strides, *lse_strides,
+                               queries, heads, 1 if causal else 0, softmax_scale)
         call = msf_cache_attend_simt if simt else msf_cache_attend
-        call(self.handle, layer, _list(seqs, n)[0], n, a, stream)
+        call(self.handle, layer, None if seqs is None else _list(seqs, n)[0], n, args, stream)
 
     def device_status(self, stream=None) -> int:
         return msf_cache_device_status(self.handle, stream)
