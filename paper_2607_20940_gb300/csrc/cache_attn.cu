@@ -134,8 +134,8 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 
 // ------------------------------------------------------------- few queries
 //
-// Up to 8 NT rows (the queries of the heads that share a key head) against a
-// sequence's tokens: bound by HBM (9/8 D bytes a token and key head, 4 D NT 8
+// Blocks of up to 8 NT rows (the queries of the heads that share a key head)
+// against a sequence's tokens: bound by HBM (9/8 D bytes a token and key head, 4 D NT 8
 // operations), and close to it by the instructions that take codes apart. A warp
 // takes a pair of records (32 tokens) at a time; for each of them
 //   scores [16 tokens x 8 rows] += K [16 x 16] Q^T, D / 16 products,
@@ -257,7 +257,10 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     __shared__ int s_merge[2];
     __shared__ int abort_flag;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-    const int rows = a.group.d * a.queries;
+    // Rows of a key head, in one or two blocks; a head's blocks are items of their own.
+    const int all_rows = a.group.d * a.queries, two = all_rows > C::kRows, n_heads = c.Hk << two;
+    auto rows_of = [&](int hb) { return two && !(hb & 1) ? C::kRows : all_rows - (two ? C::kRows : 0); };
+    auto row_of = [&](int hb, int r) { return r + (two && (hb & 1) ? C::kRows : 0); };
     unsigned char* ring = smem + warp * C::kOwn;
     auto part_of = [&](int w, int last) {  // the first piece of warp w, or its last
         return reinterpret_cast<float*>(last ? smem + w * C::kOwn : smem + kW * C::kOwn + w * C::kPart);
@@ -280,12 +283,16 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     };
     auto pairs_of = [&](int len) { return (len + 31) / 32; };
     auto units_of = [&](int len) { return len > 0 ? pairs_of(len) + kItem : 0; };
-    // Row r of (row i of the list, key head hk): its place in q, out and lse.
-    auto place = [&](const long long* st, int i, int hk, int r) {
+    // Row r of (row i of the list, head's block hb): its place in q, out and lse.
+    auto place = [&](const long long* st, int i, int hb, int r) {
+        r = row_of(hb, r);
+        const int hk = hb >> two;
         const int u = a.group.div(r);
         return i * st[0] + u * st[1] + (hk * a.group.d + r - u * a.group.d) * st[2];
     };
-    auto lse_place = [&](int i, int hk, int r) {
+    auto lse_place = [&](int i, int hb, int r) {
+        r = row_of(hb, r);
+        const int hk = hb >> two;
         const int u = a.group.div(r);
         return i * a.l_st[0] + (hk * a.group.d + r - u * a.group.d) * a.l_st[1] + u;
     };
@@ -318,25 +325,25 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         none |= x == 0;
         mine += x;
     }
-    const long long before_mine = scan(mine, U) * c.Hk;
-    U *= c.Hk;
+    const long long before_mine = scan(mine, U) * n_heads;
+    U *= n_heads;
 
     // ---- sequences without tokens: their rows are empty, or the base's
     if (__syncthreads_or(none))
-        for (long long x = blockIdx.x; x < (long long)a.n * c.Hk; x += gridDim.x) {
-            const int i = (int)(x / c.Hk), hk = (int)(x % c.Hk);
+        for (long long x = blockIdx.x; x < (long long)a.n * n_heads; x += gridDim.x) {
+            const int i = (int)(x / n_heads), hb = (int)(x % n_heads);
             if (length(i) > 0) continue;
             if (threadIdx.x == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
-            for (int y = threadIdx.x; y < rows * (D / 8); y += kT) {
+            for (int y = threadIdx.x; y < rows_of(hb) * (D / 8); y += kT) {
                 const int r = y / (D / 8), d = y % (D / 8) * 8;
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
-                    w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
-                *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+                if (a.base_out && a.base_lse[lse_place(i, hb, r)] != -INFINITY)
+                    w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hb, r) + d);
+                *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hb, r) + d) = w;
             }
             if (a.lse && a.lse != a.base_lse)
-                for (int r = threadIdx.x; r < rows; r += kT)
-                    a.lse[lse_place(i, hk, r)] = a.base_lse ? a.base_lse[lse_place(i, hk, r)] : -INFINITY;
+                for (int r = threadIdx.x; r < rows_of(hb); r += kT)
+                    a.lse[lse_place(i, hb, r)] = a.base_lse ? a.base_lse[lse_place(i, hb, r)] : -INFINITY;
         }
 
     // ---- the warps' shares. A pair belongs to the warp that has its unit: the item's
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     const int me = (int)blockIdx.x * kW + warp;
     const long long cta0 = share((int)blockIdx.x * kW);
     if (a.n <= kT) {
-        if (cta0 >= before_mine && cta0 < before_mine + mine * c.Hk) {
+        if (cta0 >= before_mine && cta0 < before_mine + mine * n_heads) {
             s_found[0] = threadIdx.x;
             s_found[1] = before_mine;
         }
@@ -356,7 +363,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         long long base = 0;
         for (int i0 = 0; i0 < a.n; i0 += kT) {
             const int i = i0 + (int)threadIdx.x;
-            const long long x = i < a.n ? (long long)units_of(length(i)) * c.Hk : 0;
+            const long long x = i < a.n ? (long long)units_of(length(i)) * n_heads : 0;
             long long all;
             const long long before = base + scan(x, all);
             if (cta0 >= before && cta0 < before + x) {
@@ -377,18 +384,19 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     bool ok = true;
     for (long long u = u0; u < u1 && ok;) {
         const int len = length(seq), n_pairs = pairs_of(len), per = units_of(len);
-        if (u >= seq0 + (long long)per * c.Hk) {
-            seq0 += (long long)per * c.Hk;
+        if (u >= seq0 + (long long)per * n_heads) {
+            seq0 += (long long)per * n_heads;
             ++seq;
             continue;
         }
-        const int hk = (int)((u - seq0) / per);
-        const long long item0 = seq0 + (long long)hk * per;
+        const int hb = (int)((u - seq0) / per);
+        const long long item0 = seq0 + (long long)hb * per;
         const int r0 = (int)max(0ll, u - item0 - kItem), r1 = (int)min((long long)n_pairs, u1 - item0 - kItem);
         u = item0 + per;
         if (r0 >= r1) continue;  // the share ends before the first pair
         const int* row = c.table + (size_t)(a.seqs ? a.seqs[seq] : seq) * c.W;
-        const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes + (long long)hk * (c.P / 16) * kRec;
+        const int rows = rows_of(hb);
+        const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes + (long long)(hb >> two) * (c.P / 16) * kRec;
         // Lanes 0 and 1 ask for a record of a pair each.
         const int n_rec = (len + 15) / 16;
         auto page_of = [&](int r) { return 2 * r + lane < n_rec && lane < 2 ? row[(2 * r + lane) >> (c.log2_p - 4)] : 0; };
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             const int r = 8 * nt + g;
             uint32_t w[D / 8];
             if (r < rows) {
-                const uint16_t* q = a.q + place(a.q_st, seq, hk, r) + t * (D / 4);
+                const uint16_t* q = a.q + place(a.q_st, seq, hb, r) + t * (D / 4);
 #pragma unroll
                 for (int e = 0; e < D / 32; ++e) {
                     const uint4 x = *reinterpret_cast<const uint4*>(q + 8 * e);
@@ -449,7 +457,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             for (int x = 0; x < 2; ++x) {
                 f[nt][x] = codes::row_factor(__shfl_sync(0xffffffffu, e, 4 * (2 * t + x)), a.scale * c.k_unit);
                 const int rr = 8 * nt + 2 * t + x;
-                limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + a.group.div(rr) : len;
+                limit[nt][x] = rr >= rows ? 0x7fffffff : a.causal ? len - a.queries + 1 + a.group.div(row_of(hb, rr)) : len;
             }
         }
         // no token below this one is hidden from a row
@@ -618,9 +626,9 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             const int first = worker_of(item0 + kItem) / kW, last = worker_of(item0 + kItem + n_pairs - 1) / kW;
             if (first < last) {
                 int* it = s_item[first < (int)blockIdx.x ? 0 : 1];
-                it[0] = seq, it[1] = hk, it[2] = first, it[3] = last - first + 1;
+                it[0] = seq, it[1] = hb, it[2] = first, it[3] = last - first + 1;
             } else if (r0 == 0) {
-                s_alone[warp][0] = seq, s_alone[warp][1] = hk;
+                s_alone[warp][0] = seq, s_alone[warp][1] = hb;
             }
         }
 #pragma unroll
@@ -634,12 +642,12 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 const int r = 8 * nt + 2 * t + e;
                 if (whole) {
                     const bool live = r < rows;
-                    const long long at = live ? lse_place(seq, hk, r) : 0;
+                    const long long at = live ? lse_place(seq, hb, r) : 0;
                     const codes::Join j = codes::join_of(m[nt][e], x, a.base_lse != nullptr, a.base_lse && live ? a.base_lse[at] : 0.f, c.v_unit);
                     __syncwarp();  // every lane has read base_lse, which may be lse
                     if (live) {
                         if (g == 0 && a.lse) a.lse[at] = j.lse;
-                        const long long out = place(a.o_st, seq, hk, r) + g * (D / 8);
+                        const long long out = place(a.o_st, seq, hb, r) + g * (D / 8);
 #pragma unroll
                         for (int i = 0; i < D / 16; i += 4) {
                             float y[8];
@@ -682,8 +690,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     if (__syncthreads_or(!ok)) return;
 
     // ---- the CTA's pieces of an item, in order
-    auto store = [&](int i, int hk, int r, int d, float4 x, float own, float other) {  // four dims of a row's result
-        const long long at = place(a.o_st, i, hk, r) + d;
+    auto store = [&](int i, int hb, int r, int d, float4 x, float own, float other) {  // four dims of a row's result
+        const long long at = place(a.o_st, i, hb, r) + d;
         x.x *= own, x.y *= own, x.z *= own, x.w *= own;
         if (other != 0.f) {
             const uint2 y = *reinterpret_cast<const uint2*>(a.base_out + at);
@@ -692,8 +700,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         }
         *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(x.x, x.y), ptx::pack_bf16(x.z, x.w));
     };
-    auto finish = [&](int i, int hk, int r, float M, float L) {  // a row's join, by one thread
-        const long long at = lse_place(i, hk, r);
+    auto finish = [&](int i, int hb, int r, float M, float L) {  // a row's join, by one thread
+        const long long at = lse_place(i, hb, r);
         const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
         if (a.lse) a.lse[at] = j.lse;
         s_own[warp][r] = j.own;
@@ -734,16 +742,16 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     // Items of this CTA alone: by the warp that has the first piece.
     int end, over = -1;  // over: the warp whose last piece's item goes on in the next CTA
     if (s_last[warp] && !extent(warp, 1, end)) {
-        const int i = s_alone[warp][0], hk = s_alone[warp][1];
+        const int i = s_alone[warp][0], hb = s_alone[warp][1], rows = rows_of(hb);
         if (lane < rows) {
             float M, L;
             weigh(warp, 1, end, lane, M, L);
-            finish(i, hk, lane, M, L);
+            finish(i, hb, lane, M, L);
         }
         __syncwarp();
         for (int x = lane; x < rows * (D / 4); x += 32) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
-            store(i, hk, r, d, sum(warp, 1, end, r, d), s_own[warp][r], s_other[warp][r]);
+            store(i, hb, r, d, sum(warp, 1, end, r, d), s_own[warp][r], s_other[warp][r]);
         }
         __syncwarp();
     }
@@ -754,6 +762,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         const int w0 = k ? over : s_first[0] ? 0 : -1;
         if (w0 < 0) continue;
         extent(w0, k, end);
+        const int rows = rows_of(s_item[k][1]);
         float* slot = c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot;
         if (threadIdx.x < rows) {
             float M, L;
@@ -781,7 +790,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     // ---- items of several CTAs that this one finished last
     for (int k = 0; k < 2; ++k) {
         if (!s_merge[k]) continue;
-        const int i = s_item[k][0], hk = s_item[k][1], first = s_item[k][2], n = s_item[k][3];
+        const int i = s_item[k][0], hb = s_item[k][1], first = s_item[k][2], n = s_item[k][3], rows = rows_of(hb);
         // a CTA's piece of an item that begins in it is in its slot 1
         auto slot_of = [&](int x) { return c.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * C::kSlot; };
         for (int r = warp; r < rows; r += kW) {
@@ -796,7 +805,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
 #pragma unroll
             for (int d = 16; d; d /= 2) L += __shfl_xor_sync(0xffffffffu, L, d);
             if (lane == 0) {
-                finish(i, hk, r, M, L);
+                finish(i, hb, r, M, L);
                 s_M[r] = M;
             }
         }
@@ -811,7 +820,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 const float4 z = __ldcg(reinterpret_cast<const float4*>(slot_of(x) + r * D + d));
                 acc.x = fmaf(w, z.x, acc.x), acc.y = fmaf(w, z.y, acc.y), acc.z = fmaf(w, z.z, acc.z), acc.w = fmaf(w, z.w, acc.w);
             }
-            store(i, hk, r, d, acc, s_own[r % kW][r], s_other[r % kW][r]);
+            store(i, hb, r, d, acc, s_own[r % kW][r], s_other[r % kW][r]);
         }
         __syncthreads();
     }
@@ -839,7 +848,7 @@ cudaError_t launch_cache_attend_simt(const CacheView& c, const CacheAttnArgs& a,
 cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
     const long long rows = (long long)a.group.d * a.queries;
     if (rows <= 8) return c.D == 128 ? launch_few<128, 1>(c, a, st) : launch_few<64, 1>(c, a, st);
-    if (rows <= 16) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
+    if (rows <= 32) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
     return launch_cache_attend_many(c, a, st);
 }
 
