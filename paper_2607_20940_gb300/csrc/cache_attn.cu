@@ -145,7 +145,9 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // exact in f16. Which of a product's 16 columns stands for which dim or token is
 // free, so each lane keeps what it loads: 32 neighbouring dims of two tokens for
 // the scores, one block of four tokens for the outputs. Pairs come through a ring
-// of bulk copies of the warp's own (no registers wait for memory).
+// of asynchronous copies of the warp's own (no registers wait for memory). Bulk
+// copies with a barrier took 600 of a pair's 3850 cycles, 16-byte copies by every
+// lane @@.
 //
 // Work: every (sequence, key head) is an item of its pairs and kItem more units
 // (what a piece costs besides them); the warps of the grid take equal, contiguous
@@ -157,7 +159,6 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kItem = 1;
-constexpr long long kWaitLimit = 2000000000LL;  // ~1 s of SM clock
 
 // c += a b, f16 in fp32.
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
@@ -240,11 +241,10 @@ static_assert(FewCfg<128, 1>::kSmem <= 226 * 1024 && FewCfg<128, 2>::kSmem <= 22
 
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
-    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_units, long long wait_limit) {
+    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_units) {
     using C = FewCfg<D, NT>;
     constexpr int kW = C::kWarps, kT = 32 * kW, kS = C::kStages, kRec = cache_record_bytes(D);
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ uint64_t full[kW][kS];
     __shared__ float s_w[2][kW][C::kRows];                 // weights of the warps' first and last pieces
     __shared__ float s_own[kW][C::kRows], s_other[kW][C::kRows];  // an item's join, by the warp that adds it
     __shared__ float s_M[C::kRows];
@@ -255,7 +255,6 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     __shared__ int s_alone[kW][2];  // of a last piece whose item is this CTA's alone: row of the list, head
     __shared__ int s_item[2][4];    // items of several CTAs, begun before this one and in it: row, head, first CTA, CTAs
     __shared__ int s_merge[2];
-    __shared__ int abort_flag;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     // Rows of a key head, in one or two blocks; a head's blocks are items of their own.
     const int all_rows = a.group.d * a.queries, two = all_rows > C::kRows, n_heads = c.Hk << two;
@@ -265,15 +264,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     auto part_of = [&](int w, int last) {  // the first piece of warp w, or its last
         return reinterpret_cast<float*>(last ? smem + w * C::kOwn : smem + kW * C::kOwn + w * C::kPart);
     };
-    if (threadIdx.x == 0) abort_flag = 0;
     if (threadIdx.x < 2) s_merge[threadIdx.x] = 0;
-    if (lane == 0) {
-        for (int s = 0; s < kS; ++s) ptx::mbar_init(&full[warp][s], 1);
-        ptx::fence_mbar_init();
-        s_first[warp] = s_last[warp] = 0;
-    }
-    __syncthreads();
-    volatile int* abort_p = &abort_flag;
+    if (lane == 0) s_first[warp] = s_last[warp] = 0;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
@@ -348,10 +340,10 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
 
     // ---- the warps' shares. A pair belongs to the warp that has its unit: the item's
     // first + kItem + pair; the CTA finds the sequence that its first warp begins in.
-    const int workers = (int)min((long long)gridDim.x * kW, max(1ll, U / min_units));
+    const int workers = (int)min((long long)gridDim.x * kW, max(1ll, codes::divide(U, min_units)));
     if ((int)blockIdx.x * kW >= workers || U == 0) return;
-    auto share = [&](int w) { return w >= workers ? U : (long long)((unsigned long long)U * w / workers); };
-    auto worker_of = [&](long long u) { return (int)(((u + 1) * workers - 1) / U); };
+    auto share = [&](int w) { return w >= workers ? U : codes::divide(U * w, workers); };
+    auto worker_of = [&](long long u) { return (int)codes::divide((u + 1) * workers - 1, U); };
     const int me = (int)blockIdx.x * kW + warp;
     const long long cta0 = share((int)blockIdx.x * kW);
     if (a.n <= kT) {
@@ -380,16 +372,14 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     const long long u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
     int seq = (int)s_found[0];
     long long seq0 = s_found[1];  // first unit of the sequence
-    int issued = 0, taken = 0;    // pairs asked for and used, over all pieces
-    bool ok = true;
-    for (long long u = u0; u < u1 && ok;) {
+    for (long long u = u0; u < u1;) {
         const int len = length(seq), n_pairs = pairs_of(len), per = units_of(len);
         if (u >= seq0 + (long long)per * n_heads) {
             seq0 += (long long)per * n_heads;
             ++seq;
             continue;
         }
-        const int hb = (int)((u - seq0) / per);
+        const int hb = (int)codes::divide(u - seq0, per);
         const long long item0 = seq0 + (long long)hb * per;
         const int r0 = (int)max(0ll, u - item0 - kItem), r1 = (int)min((long long)n_pairs, u1 - item0 - kItem);
         u = item0 + per;
@@ -397,28 +387,38 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         const int* row = c.table + (size_t)(a.seqs ? a.seqs[seq] : seq) * c.W;
         const int rows = rows_of(hb);
         const uint8_t* pool = c.pool + (long long)a.layer * c.pages * c.page_bytes + (long long)(hb >> two) * (c.P / 16) * kRec;
-        // Lanes 0 and 1 ask for a record of a pair each.
+        // A lane copies every 32nd 16 bytes of a pair. Pages: of its two records.
         const int n_rec = (len + 15) / 16;
-        auto page_of = [&](int r) { return 2 * r + lane < n_rec && lane < 2 ? row[(2 * r + lane) >> (c.log2_p - 4)] : 0; };
-        auto fetch = [&](int r, int page) {
-            const int st = issued % kS, x = 2 * r + lane;
-            ++issued;
-            if (lane == 0) ptx::mbar_arrive_expect_tx(&full[warp][st], (uint32_t)(min(2, n_rec - 2 * r) * kRec));
-            __syncwarp();
-            if (lane < 2 && x < n_rec) {
+        auto pages_of = [&](int r) {
+            const int sh = c.log2_p - 4;
+            return 2 * r + 1 < n_rec ? make_int2(row[(2 * r) >> sh], row[(2 * r + 1) >> sh]) : make_int2(row[(2 * r) >> sh], -1);
+        };
+        auto fetch = [&](int r, int2 page, int st) {
+            auto from = [&](int pg, int x) {
                 // a page number from outside is read as page 0, like any stale page
-                const long long at = cache_page_ok(c, page) ? page : 0;
-                ptx::bulk_load(ring + (2 * st + lane) * kRec, pool + at * c.page_bytes + (x & (c.P / 16 - 1)) * kRec, kRec, &full[warp][st]);
+                const long long at = cache_page_ok(c, pg) ? pg : 0;
+                return pool + at * c.page_bytes + (x & (c.P / 16 - 1)) * kRec + lane * 16;
+            };
+            const bool both = 2 * r + 1 < n_rec;
+            const uint8_t* p0 = from(page.x, 2 * r);
+            const uint8_t* p1 = from(page.y, 2 * r + 1) - kRec;
+            const uint32_t to = ptx::smem_u32(ring) + st * 2 * kRec + lane * 16;
+#pragma unroll
+            for (int k = 0; k < (2 * kRec + 511) / 512; ++k) {
+                const bool second = 512 * k + 16 * lane >= kRec;
+                if ((!second || both) && 512 * k + 16 * lane < 2 * kRec) ptx::async_copy16(to + 512 * k, (second ? p1 : p0) + 512 * k);
             }
         };
         int next = r0;  // pair to ask for
 #pragma unroll
-        for (int s = 0; s < kS; ++s)
+        for (int s = 0; s < kS; ++s) {
             if (next < r1) {
-                fetch(next, page_of(next));
+                fetch(next, pages_of(next), s);
                 ++next;
             }
-        int page_next = next < r1 ? page_of(next) : 0;
+            ptx::async_commit();
+        }
+        int2 page_next = next < r1 ? pages_of(next) : make_int2(0, 0);
 
         // ---- queries: row g + 8 nt, dims D / 4 t ...
         uint32_t qf[NT][D / 16][2];
@@ -474,10 +474,9 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
         }
         for (int r = r0; r < r1; ++r) {
-            const int st = taken % kS;
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp][st], (uint32_t)(taken / kS & 1), abort_p, wait_limit));
-            if (!ok) break;
-            ++taken;
+            const int st = (r - r0) % kS;
+            ptx::async_wait<kS - 1>();
+            __syncwarp();
             const uint8_t* pair = ring + 2 * st * kRec;
             float s[2][NT][4];
 #pragma unroll
@@ -608,11 +607,11 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             // every lane has its part of the pair
             __syncwarp();
             if (next < r1) {
-                fetch(next, page_next);
-                if (++next < r1) page_next = page_of(next);
+                fetch(next, page_next, st);
+                if (++next < r1) page_next = pages_of(next);
             }
+            ptx::async_commit();
         }
-        if (!ok) break;
 
         // ---- the piece's result
         const bool whole = r0 == 0 && r1 == n_pairs;
@@ -680,14 +679,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             }
         __syncwarp();
     }
-    if (!ok) {
-        // every copy asked for lands before its space goes
-        volatile int never = 0;
-        for (int i = taken; i < issued; ++i)
-            ptx::mbar_wait_bounded(&full[warp][i % kS], (uint32_t)(i / kS & 1), &never, kWaitLimit);
-        if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
-    }
-    if (__syncthreads_or(!ok)) return;
+    __syncthreads();
 
     // ---- the CTA's pieces of an item, in order
     auto store = [&](int i, int hb, int r, int d, float4 x, float own, float other) {  // four dims of a row's result
@@ -834,7 +826,7 @@ cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t 
     if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(cache_few_kernel<D, NT>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
-                      st, c, a, 2, kWaitLimit);
+                      st, c, a, 2);
 }
 
 }  // namespace

@@ -62,6 +62,12 @@ __device__ __forceinline__ float row_factor(int e, float scale) {
     return fminf(fmaxf(row_down(e) * scale * 1.4426950408889634f, 1.17549435e-38f), 3.0e38f);
 }
 
+// n / d, by a 32-bit division where n allows it (a 64-bit one takes hundreds of cycles).
+__device__ __forceinline__ long long divide(long long n, long long d) {
+    if (((unsigned long long)n | (unsigned long long)d) >> 32) return (long long)((unsigned long long)n / (unsigned long long)d);
+    return (long long)((unsigned)n / (unsigned)d);
+}
+
 // The joined result's weights: this attention's unnormalised output times own,
 // the base's times other. M: running maximum (base 2), L: sum.
 struct Join {

@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     U *= c.Hk;
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
     const bool idle = (int)blockIdx.x >= G || U == 0;
-    const long long u0 = idle ? 0 : U * blockIdx.x / G, u1 = idle ? 0 : U * (blockIdx.x + 1) / G;
+    const long long u0 = idle ? 0 : codes::divide(U * blockIdx.x, G), u1 = idle ? 0 : codes::divide(U * (blockIdx.x + 1), G);
     if (a.n <= kThreads) {
         if (!idle && u0 >= before_mine && u0 < before_mine + mine * c.Hk) {
             s_found[0] = threadIdx.x;
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const int len = shape.length((int)s_found[0]);
         long long per;
         const long long before = scan((int)threadIdx.x < shape.blocks ? shape.units(len, threadIdx.x) : 0, per);
-        const long long in = u0 - s_found[1], hk = in / per, rest = in - hk * per;
+        const long long in = u0 - s_found[1], hk = codes::divide(in, per), rest = in - hk * per;
         if ((int)threadIdx.x < shape.blocks && rest >= before && rest < before + shape.units(len, threadIdx.x)) {
             s_begin[0] = (int)hk;
             s_begin[1] = threadIdx.x;
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             if (!whole) {
                 const long long all = s_units[0], u = s_units[1] + pc.item0 + kItem;
                 const int ctas = (int)min((long long)gridDim.x, max(1ll, all / 2));
-                auto cta_of = [&](long long v) { return (int)(((v + 1) * ctas - 1) / all); };
+                auto cta_of = [&](long long v) { return (int)codes::divide((v + 1) * ctas - 1, all); };
                 const int first = cta_of(u), n = cta_of(u + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
                 ptx::named_bar_sync(1, 256);
                 if (threadIdx.x == 256) {
