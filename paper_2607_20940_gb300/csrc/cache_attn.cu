@@ -692,89 +692,85 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         }
         *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(x.x, x.y), ptx::pack_bf16(x.z, x.w));
     };
-    auto finish = [&](int i, int hb, int r, float M, float L) {  // a row's join, by one thread
+    auto finish = [&](int at_warp, int i, int hb, int r, float M, float L) {  // a row's join, by one thread
         const long long at = lse_place(i, hb, r);
         const codes::Join j = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
         if (a.lse) a.lse[at] = j.lse;
-        s_own[warp][r] = j.own;
-        s_other[warp][r] = j.other;
+        s_own[at_warp][r] = j.own;
+        s_other[at_warp][r] = j.other;
     };
-    // An item's pieces begin with warp w0's last, or with the CTA's first; the others
-    // are the first pieces of the warps after it, up to `end`. Returns whether the
-    // item goes on in the next CTA.
+    // The pieces of an item (a group): warp w0's last, or the CTA's first, and then the
+    // first pieces of the warps after it up to `end`. Whether the item goes on in the next CTA.
     auto extent = [&](int w0, int last, int& end) {
         end = w0;
         bool goes_on = last ? true : s_first[w0] == 2;
         while (goes_on && end + 1 < kW) goes_on = s_first[++end] == 2;
         return goes_on;
     };
-    // Row r's maximum and sum over them; their weights into s_w.
-    auto weigh = [&](int w0, int last, int end, int r, float& M, float& L) {
-        auto ml_of = [&](int w) {
-            return *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * r);
-        };
-        M = kLowest, L = 0.f;
-        for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w).x);
-        for (int w = w0; w <= end; ++w) {
-            const float2 x = ml_of(w);
-            const float k = codes::ex2(x.x - M);
-            s_w[last && w == w0][w][r] = k;
-            L += k * x.y;
-        }
-    };
-    auto sum = [&](int w0, int last, int end, int r, int d) {
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int w = w0; w <= end; ++w) {
-            const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == w0) + r * C::kPitch + d);
-            const float k = s_w[last && w == w0][w][r];
-            y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
-        }
-        return y;
-    };
-    // Items of this CTA alone: by the warp that has the first piece.
-    int end, over = -1;  // over: the warp whose last piece's item goes on in the next CTA
-    if (s_last[warp] && !extent(warp, 1, end)) {
-        const int i = s_alone[warp][0], hb = s_alone[warp][1], rows = rows_of(hb);
-        if (lane < rows) {
-            float M, L;
-            weigh(warp, 1, end, lane, M, L);
-            finish(i, hb, lane, M, L);
-        }
-        __syncwarp();
-        for (int x = lane; x < rows * (D / 4); x += 32) {
-            const int r = x / (D / 4), d = x % (D / 4) * 4;
-            store(i, hb, r, d, sum(warp, 1, end, r, d), s_own[warp][r], s_other[warp][r]);
-        }
-        __syncwarp();
-    }
-    // Items of several CTAs: by the whole CTA, into its slots.
-    for (int w = 0; w < kW; ++w)
-        if (s_last[w] && extent(w, 1, end)) over = w;
-    for (int k = 0; k < 2; ++k) {
-        const int w0 = k ? over : s_first[0] ? 0 : -1;
-        if (w0 < 0) continue;
-        extent(w0, k, end);
-        const int rows = rows_of(s_item[k][1]);
-        float* slot = c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot;
-        if (threadIdx.x < rows) {
-            float M, L;
-            weigh(w0, k, end, threadIdx.x, M, L);
-            __stcg(reinterpret_cast<float2*>(slot + C::kRows * D + 2 * threadIdx.x), make_float2(M, L));
-        }
-        __syncthreads();
-        for (int x = threadIdx.x; x < rows * (D / 4); x += kT) {
-            const int r = x / (D / 4), d = x % (D / 4) * 4;
-            __stcg(reinterpret_cast<float4*>(slot + r * D + d), sum(w0, k, end, r, d));
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const int* it = s_item[k];
-            __threadfence();
-            s_merge[k] = atomicAdd(c.counters + it[2], 1u) == (unsigned)it[3] - 1;
-            if (s_merge[k]) {
-                c.counters[it[2]] = 0;  // for the next launch
-                __threadfence();
+    auto slot_at = [&](int k) { return c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot; };
+    // A warp weighs a group's pieces, a lane a row: into s_w, and what the whole group
+    // has into the item's join, or (items of several CTAs) into the CTA's slot.
+    auto weigh = [&](int w0, int last) {
+        int end;
+        const bool alone = !extent(w0, last, end) && last;
+        const int i = alone ? s_alone[w0][0] : s_item[last][0], hb = alone ? s_alone[w0][1] : s_item[last][1];
+        if (lane < rows_of(hb)) {
+            auto ml_of = [&](int w) {
+                return *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * lane);
+            };
+            float M = kLowest, L = 0.f;
+#pragma unroll 4
+            for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w).x);
+#pragma unroll 4
+            for (int w = w0; w <= end; ++w) {
+                const float2 x = ml_of(w);
+                const float k = codes::ex2(x.x - M);
+                s_w[last && w == w0][w][lane] = k;
+                L += k * x.y;
             }
+            if (alone)
+                finish(w0, i, hb, lane, M, L);
+            else
+                __stcg(reinterpret_cast<float2*>(slot_at(last) + C::kRows * D + 2 * lane), make_float2(M, L));
+        }
+    };
+    if (s_last[warp]) weigh(warp, 1);
+    if (warp == kW - 1 && s_first[0]) weigh(0, 0);
+    __syncthreads();
+    // The whole CTA adds them, a thread four dims of a row. over: the group whose item goes on.
+    int over = -1;
+    // groups: bit 0 the one that the CTA begins with, bit w + 1 the one of warp w's last piece
+    unsigned groups = (__ballot_sync(0xffffffffu, lane < kW && s_last[lane < kW ? lane : 0]) << 1) | (s_first[0] ? 1u : 0u);
+    for (; groups; groups &= groups - 1) {
+        const int w0 = __ffs(groups) - 2, last = w0 >= 0, from = last ? w0 : 0;
+        int end;
+        const bool goes_on = extent(from, last, end), alone = last && !goes_on;
+        if (last && goes_on) over = w0;
+        const int i = alone ? s_alone[from][0] : s_item[last][0], hb = alone ? s_alone[from][1] : s_item[last][1];
+        for (int x = threadIdx.x; x < rows_of(hb) * (D / 4); x += kT) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int w = from; w <= end; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == from) + r * C::kPitch + d);
+                const float k = s_w[last && w == from][w][r];
+                y.x = fmaf(k, z.x, y.x), y.y = fmaf(k, z.y, y.y), y.z = fmaf(k, z.z, y.z), y.w = fmaf(k, z.w, y.w);
+            }
+            if (alone)
+                store(i, hb, r, d, y, s_own[from][r], s_other[from][r]);
+            else
+                __stcg(reinterpret_cast<float4*>(slot_at(last) + r * D + d), y);
+        }
+    }
+    __syncthreads();
+    // Items of several CTAs: this one's pieces are in place.
+    if (lane == 0 && warp < 2 && (warp ? over >= 0 : s_first[0] != 0)) {
+        const int* it = s_item[warp];
+        __threadfence();
+        s_merge[warp] = atomicAdd(c.counters + it[2], 1u) == (unsigned)it[3] - 1;
+        if (s_merge[warp]) {
+            c.counters[it[2]] = 0;  // for the next launch
+            __threadfence();
         }
     }
     __syncthreads();
@@ -797,7 +793,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
 #pragma unroll
             for (int d = 16; d; d /= 2) L += __shfl_xor_sync(0xffffffffu, L, d);
             if (lane == 0) {
-                finish(i, hb, r, M, L);
+                finish(warp, i, hb, r, M, L);
                 s_M[r] = M;
             }
         }
