@@ -148,6 +148,9 @@ typedef struct msf_cache_attention {
     int32_t heads;            /* a multiple of kv_heads: heads/kv_heads neighbours share keys and values */
     int32_t causal;           /* 0: every query sees the whole sequence; 1: query i sees its first
                                  length - queries + 1 + i tokens (the queries are its newest tokens) */
+    int32_t skip;             /* newest tokens of every sequence that are not seen (>= 0): as if it
+                                 were that much shorter. A layer's frame can so be written into room
+                                 that all layers of it got at once */
     float softmax_scale;      /* 0: 1/sqrt(D) */
 } msf_cache_attention;
 

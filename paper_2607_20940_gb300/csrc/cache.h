@@ -106,7 +106,7 @@ struct CacheAttnArgs {
     long long q_st[3], o_st[3], l_st[2];
     int queries, heads;
     FastDiv group;  // heads / Hk
-    int causal;
+    int causal, skip;
     int layer, n;
     const int* seqs;
     float scale;

@@ -214,7 +214,7 @@ static msf_status attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, 
     // seqs may repeat here, so n is not bounded by the cache's sequences, unless it stands for 0..n-1
     if (n < 0 || (!seqs && n > cache->d.sequences) || !aligned4(seqs)) return MSF_ERR_INVALID_ARG;
     if (x.queries < 0 || x.heads < 1 || x.heads % cache->d.kv_heads) return MSF_ERR_INVALID_ARG;
-    if (x.causal != 0 && x.causal != 1) return MSF_ERR_INVALID_ARG;
+    if ((x.causal != 0 && x.causal != 1) || x.skip < 0) return MSF_ERR_INVALID_ARG;
     if (!(x.softmax_scale >= 0.f) || !isfinite(x.softmax_scale)) return MSF_ERR_INVALID_ARG;
     if (!strides_ok(x.q_strides) || !strides_ok(x.out_strides)) return MSF_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i)
@@ -240,6 +240,7 @@ static msf_status attend(msf_cache_t cache, int32_t layer, const int32_t* seqs, 
     a.heads = x.heads;
     a.group = msf::FastDiv(x.heads / cache->d.kv_heads);
     a.causal = x.causal;
+    a.skip = x.skip;
     a.layer = layer;
     a.n = n;
     a.seqs = seqs;

@@ -85,7 +85,7 @@ struct Shape {
         : c(c_), a(a_), rows(a_.group.d * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
     __device__ int length(int i) const {
         const int s = a.seqs ? a.seqs[i] : i;
-        return (unsigned)s < (unsigned)c.S ? min(max(c.lengths[s], 0), c.W * c.P) : 0;
+        return (unsigned)s < (unsigned)c.S ? max(0, min(c.lengths[s], c.W * c.P) - a.skip) : 0;
     }
     __device__ int block_rows(int b) const { return min(kBlock, rows - b * kBlock); }
     __device__ int tiles(int b) const { return (block_rows(b) + kTile - 1) / kTile; }

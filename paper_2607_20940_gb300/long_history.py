@@ -1,0 +1,157 @@
+"""Streams that remember every frame: the window pass with its history in 4 bits.
+
+The history ring of a plan holds a few bf16 frames. `LongHistory` keeps all frames that a
+stream has emitted in one paged 4-bit cache (`msf.Cache`) instead: a sequence for every
+(stream, scale of the window), so that a query group of scale g finds the history already
+subsampled to g, and all layers of a frame in the same pages. A layer's attention is then
+two calls, joined by the rows' log-sum-exp: the plan's attention over sink and window, and
+the cache's over the history, in place (Eq. 4's softmax over sink, history and window).
+
+Streams can branch from one another (they share the pages of their common past), forget
+their oldest or newest frames, and end; the pages of what is gone can be drawn together.
+
+    python -m paper_2607_20940_gb300.long_history     # a small rollout with a branch
+"""
+from __future__ import annotations
+
+from typing import Sequence
+
+import torch
+
+from . import msf
+
+
+class LongHistory:
+    """Window plans of `layers` layers and the 4-bit history of up to `streams` streams.
+
+    scales, grid_h, grid_w, heads, head_dim, sink_tokens: as msf.make_desc, with scales[0] == 1
+    (emitted frames are fine). batch: streams of a window pass. frames: history frames that the
+    pool holds in all, over all streams; stream_frames: of one stream at most."""
+
+    def __init__(self, scales: Sequence[int], grid_h: int, grid_w: int, heads: int, head_dim: int, sink_tokens: int,
+                 layers: int = 1, batch: int = 1, streams: int = 1, frames: int = 64, stream_frames: int = 64,
+                 page_tokens: int = 64, device="cuda"):
+        if scales[0] != 1:
+            raise ValueError("the head state is a fine one: scales[0] is 1")
+        desc = msf.make_desc(scales, grid_h, grid_w, heads, head_dim, sink_tokens, 0, batch=batch)
+        self.scales = tuple(scales)
+        self.plans = [msf.Plan(desc) for _ in range(layers)]
+        self.info = self.plans[0].info
+        self.groups = [self.info.groups[i] for i in range(self.info.n_groups)]
+        self.batch, self.streams, self.device = batch, streams, device
+        self.counts = [self.info.fine_tokens // (g.scale * g.scale) for g in self.groups]  # tokens of a frame
+        need = lambda n, k: -(-n * k // page_tokens)  # noqa: E731
+        # a branch has a last page of its own in every group
+        pages = sum(need(n, frames) for n in self.counts) + len(self.groups) * streams
+        self.cache = msf.Cache(msf.make_cache_desc(layers, heads, head_dim, page_tokens, pages,
+                                                   streams * len(self.groups), need(max(self.counts), stream_frames)))
+        self.cache.bind(self.cache.pool(device), self.cache.state(device), self.cache.workspace(device))
+        self.workspace = self.plans[0].workspace(device)  # the layers' calls follow one another
+
+    def bind_sink(self, layer: int, k_sink, v_sink):
+        """The layer's sink [batch, sink_tokens, heads, head_dim] (None without one)."""
+        self.plans[layer].bind(self.workspace, k_sink, v_sink, None, None)
+
+    def rows(self, streams, group: int):
+        """Sequences of the listed streams in a query group, as a device list."""
+        return torch.tensor([s * len(self.groups) + group for s in streams], dtype=torch.int32, device=self.device)
+
+    def window(self, streams):
+        """The streams of a window pass (one of the batch each), once a pass: what the calls below take."""
+        if len(streams) != self.batch:
+            raise ValueError(f"{len(streams)} streams, where the plans have a batch of {self.batch}")
+        seqs = [self.rows(streams, i) for i in range(len(self.groups))]
+        return seqs, torch.cat(seqs), torch.tensor([n for n in self.counts for _ in streams], dtype=torch.int32,
+                                                   device=self.device)
+
+    def attend(self, layer: int, window, q, k_win, v_win, out, lse, emitting=False):
+        """Attention of a layer: q, k_win, v_win, out bf16 [batch, N, heads, head_dim], lse fp32
+        [batch, heads, N] (both written). emitting: after `emit`; the frame's room is not seen."""
+        plan = self.plans[layer]
+        plan.kv_resample(k_win, v_win)
+        plan.mssa_forward_lse(q, k_win, v_win, out, lse)
+        for g, seqs, count in zip(self.groups, window[0], self.counts):
+            a, z = g.q_begin, g.q_end
+            o, ls = out[:, a:z], lse[:, :, a:z]
+            self.cache.attend(layer, q[:, a:z], o, ls, o, ls, seqs, skip=count if emitting else 0)
+
+    def emit(self, window):
+        """Room for the frame that the pass emits, in every layer and scale, before its first layer. Each layer
+        then attends and is appended."""
+        self.cache.grow(window[1], window[2])
+
+    def append(self, layer: int, window, k_win, v_win):
+        """The head state's keys and values into the history. A coarser group takes them as the layer's last
+        `attend` subsampled them."""
+        plan, n = self.plans[layer], self.counts[0]
+        for g, seqs, count in zip(self.groups, window[0], self.counts):
+            if g.scale == 1:
+                k, v = k_win[:, :n], v_win[:, :n]
+            else:
+                k, v = (self._pyramid(plan, at, g, count) for at in (plan.info.pyramid_k_offset, plan.info.pyramid_v_offset))
+            self.cache.write(layer, k, v, seqs)
+
+    def _pyramid(self, plan, offset, g, count):
+        """The head subsampled to group g's scale: the first frame of its part of the layer's pyramid."""
+        d, row = plan.desc, plan.desc.heads * plan.desc.head_dim
+        all_rows = self.workspace[int(offset):int(offset) + 2 * d.batch * plan.info.pyramid_tokens * row]
+        return all_rows.view(torch.bfloat16).view(d.batch, plan.info.pyramid_tokens, d.heads, d.head_dim)[
+            :, g.pyr_offset:g.pyr_offset + count]
+
+    def branch(self, source, target):
+        """Streams target[i] go on from streams source[i]; the common past is held once."""
+        for i in range(len(self.groups)):
+            self.cache.fork(self.rows(source, i), self.rows(target, i))
+
+    def rewind(self, streams, frames):
+        """The streams keep their first frames[i] frames."""
+        for i, n in enumerate(self.counts):
+            keep = torch.tensor([n * f for f in frames], dtype=torch.int32, device=self.device)
+            self.cache.truncate(self.rows(streams, i), keep)
+
+    def end(self, streams):
+        """The streams' history is gone; its pages move together with `self.cache.compact()`."""
+        for i in range(len(self.groups)):
+            self.cache.truncate(self.rows(streams, i))
+
+    def check(self):
+        """Synchronise, and raise what the device found."""
+        for plan in self.plans:
+            msf._check(plan.device_status(), "window pass")
+        msf._check(self.cache.device_status(), "history")
+
+
+def main():
+    scales, gh, gw, heads, dim, sink, layers = (1, 1, 2), 16, 16, 4, 64, 64, 2
+    torch.manual_seed(0)
+    h = LongHistory(scales, gh, gw, heads, dim, sink, layers, batch=2, streams=3, frames=40, stream_frames=16,
+                    page_tokens=32)
+    rand = lambda *shape: torch.randn(*shape, device="cuda").to(torch.bfloat16)  # noqa: E731
+    for layer in range(layers):
+        h.bind_sink(layer, rand(2, sink, heads, dim), rand(2, sink, heads, dim))
+    n = h.info.n_tokens
+    out, lse = torch.empty(2, n, heads, dim, dtype=torch.bfloat16, device="cuda"), torch.empty(2, heads, n, device="cuda")
+
+    def step(streams):
+        w = h.window(streams)
+        h.emit(w)
+        for layer in range(layers):
+            q, k, v = rand(2, n, heads, dim), rand(2, n, heads, dim), rand(2, n, heads, dim)
+            h.attend(layer, w, q, k, v, out, lse, emitting=True)
+            h.append(layer, w, k, v)
+
+    for _ in range(6):
+        step([0, 1])
+    h.branch([0], [2])
+    for _ in range(3):
+        step([2, 1])
+    h.end([0])
+    h.cache.compact()
+    h.check()
+    held = int((h.cache.refs > 0).sum())
+    print(f"tokens of (stream, scale): {h.cache.lengths.tolist()}; pages in use {held} of {h.cache.desc.pages}, "
+          f"{held * h.cache.info.page_bytes * layers / 1e6:.2f} MB")
+
+
+if __name__ == "__main__":
+    main()

@@ -117,7 +117,7 @@ class msf_cache_attention(ctypes.Structure):
         ("base_out", ctypes.c_void_p), ("base_lse", ctypes.c_void_p),
         ("q_strides", ctypes.c_int64 * 3), ("out_strides", ctypes.c_int64 * 3),
         ("lse_strides", ctypes.c_int64 * 2), ("queries", ctypes.c_int32), ("heads", ctypes.c_int32),
-        ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("causal", ctypes.c_int32), ("skip", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
     ]
 
 
@@ -439,7 +439,7 @@ def _rows(t, dtype, name, shape=None):
 
 
 _STRIDES = struct.Struct("@3q")
-_ATTENTION = struct.Struct("@5P3q3q2q3if")
+_ATTENTION = struct.Struct("@5P3q3q2q4if0q")
 assert _ATTENTION.size == ctypes.sizeof(msf_cache_attention)
 
 
@@ -728,9 +728,10 @@ class Cache:
         msf_cache_compact(self.handle, stream)
 
     def attend(self, layer, q, out, lse=None, base_out=None, base_lse=None, seqs=None, causal=False,
-               softmax_scale=0.0, stream=None, simt=False):
+               softmax_scale=0.0, stream=None, simt=False, skip=0):
         """Attention of q [rows, queries, heads, head_dim] over the listed sequences, joined with
-        (base_out, base_lse) where given; lse [rows, heads, queries]. simt: on fp32 CUDA cores."""
+        (base_out, base_lse) where given; lse [rows, heads, queries]. skip: newest tokens that are not
+        seen. simt: on fp32 CUDA cores."""
         torch = _torch or _get_torch()
         shape = q.shape
         if len(shape) != 4 or shape[3] != self.head_dim:
@@ -751,7 +752,7 @@ class Cache:
         args = _ATTENTION.pack(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                                0 if base_out is None else base_out.data_ptr(),
                                0 if base_lse is None else base_lse.data_ptr(), *q_strides, *strides, *lse_strides,
-                               queries, heads, 1 if causal else 0, softmax_scale)
+                               queries, heads, 1 if causal else 0, skip, softmax_scale)
         call = msf_cache_attend_simt if simt else msf_cache_attend
         call(self.handle, layer, None if seqs is None else _list(seqs, n)[0], n, args, stream)
 

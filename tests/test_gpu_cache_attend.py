@@ -255,13 +255,29 @@ def test_another_stream_and_graph():
     assert torch.equal(again, want)
 
 
+@pytest.mark.parametrize("queries", [1, 5, 140])
+def test_newest_tokens_that_are_not_seen(queries):
+    lens = [40, 7, 0, 300]
+    c = make(kv_heads=2, head_dim=64, sequences=4, pages=60, sequence_pages=24)
+    kh, vh = fill(c, lens, 30)
+    q = rows((4, queries, 4, 64), 31)
+    for causal in (False, True):
+        for simt in (False, True):
+            out, lse = torch.empty_like(q), torch.empty(4, 4, queries, device="cuda")
+            c.attend(0, q, out, lse, causal=causal, skip=16, simt=simt)
+            c.truncate(None, ints([max(0, n - 16) for n in lens]))
+            want, want_lse = check(c, kh, vh, [max(0, n - 16) for n in lens], q, causal, simt=simt)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+            c.grow(None, ints([n - max(0, n - 16) for n in lens]))  # the same pages again
+
+
 def test_refusals():
     c = make(kv_heads=2, head_dim=64)
     q = rows((4, 3, 4, 64), 1)
     out, lse = torch.empty_like(q), torch.empty(4, 4, 3, device="cuda")
     bad = [lambda: c.attend(1, q, out), lambda: c.attend(0, q[:, :, :3], out[:, :, :3]),
            lambda: c.attend(0, q, out, lse, base_out=q), lambda: c.attend(0, q, out, lse, base_lse=lse),
-           lambda: c.attend(0, q, out, softmax_scale=-1.0), lambda: c.attend(0, q, out, softmax_scale=math.nan),
+           lambda: c.attend(0, q, out, softmax_scale=-1.0), lambda: c.attend(0, q, out, softmax_scale=math.nan), lambda: c.attend(0, q, out, skip=-1),
            lambda: c.attend(0, rows((5, 3, 4, 64), 1), rows((5, 3, 4, 64), 1)),
            lambda: c.attend(0, rows((4, 3, 4, 68), 1)[..., 4:], out)]
     for call in bad:
