@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // adds theirs in order (the same bits whichever is last).
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kItem = 1;
+constexpr int kItem = 1, kSplit = 4;
 
 // c += a b, f16 in fp32.
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
@@ -228,7 +228,7 @@ __device__ __forceinline__ void operand(uint32_t (&a)[4], uint32_t w0, uint32_t 
 template <int D, int NT>
 struct FewCfg {
     static constexpr int kRows = 8 * NT;
-    static constexpr int kWarps = NT == 1 ? 16 : 12;
+    static constexpr int kWarps = NT == 1 || D == 64 ? 16 : 12;
     static constexpr int kStages = 2;  // pairs of records in flight
     static constexpr int kPitch = D + 4;                        // floats of a row of outputs in shared memory
     static constexpr int kPart = kRows * (kPitch + 2) * 4;      // a piece's output, maxima and sums
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     __shared__ int s_first[kW], s_last[kW];
     __shared__ int s_alone[kW][2];  // of a last piece whose item is this CTA's alone: row of the list, head
     __shared__ int s_item[2][4];    // items of several CTAs, begun before this one and in it: row, head, first CTA, CTAs
-    __shared__ int s_merge[2];
+    __shared__ int s_merge[2], s_most[kW];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     // Rows of a key head, in one or two blocks; a head's blocks are items of their own.
     const int all_rows = a.group.d * a.queries, two = all_rows > C::kRows, n_heads = c.Hk << two;
@@ -312,13 +312,18 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     // ---- all units, and those before each sequence of the first kT
     long long U = 0, mine = 0;
     bool none = false;
+    int most = 0;  // units of the longest item
     for (int i = threadIdx.x; i < a.n; i += kT) {
         const int x = units_of(length(i));
         none |= x == 0;
         mine += x;
+        most = max(most, x);
     }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) s_most[warp] = most;
     const long long before_mine = scan(mine, U) * n_heads;
     U *= n_heads;
+    for (int w = 0; w < kW; ++w) most = max(most, s_most[w]);
 
     // ---- sequences without tokens: their rows are empty, or the base's
     if (__syncthreads_or(none))
@@ -340,38 +345,53 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
 
     // ---- the warps' shares. A pair belongs to the warp that has its unit: the item's
     // first + kItem + pair; the CTA finds the sequence that its first warp begins in.
+    // Few items: one for a CTA, if its warps are done with the longest before an even
+    // split over all CTAs and its merge (that takes as long as kSplit pairs a warp).
+    const bool whole_items = (long long)a.n * n_heads <= gridDim.x && most <= codes::divide(U, gridDim.x) + kSplit * kW;
     const int workers = (int)min((long long)gridDim.x * kW, max(1ll, codes::divide(U, min_units)));
-    if ((int)blockIdx.x * kW >= workers || U == 0) return;
-    auto share = [&](int w) { return w >= workers ? U : codes::divide(U * w, workers); };
     auto worker_of = [&](long long u) { return (int)codes::divide((u + 1) * workers - 1, U); };
-    const int me = (int)blockIdx.x * kW + warp;
-    const long long cta0 = share((int)blockIdx.x * kW);
-    if (a.n <= kT) {
-        if (cta0 >= before_mine && cta0 < before_mine + mine * n_heads) {
-            s_found[0] = threadIdx.x;
-            s_found[1] = before_mine;
-        }
+    int seq;
+    long long seq0, u0, u1;  // first unit of the sequence; the warp's units
+    if (whole_items) {
+        if ((int)blockIdx.x >= a.n * n_heads) return;
+        seq = (int)blockIdx.x / n_heads;
+        const int len = length(seq), n = pairs_of(len);
+        seq0 = -(long long)((int)blockIdx.x % n_heads) * units_of(len);
+        // the pairs' warps are neighbours: with few, the first ones
+        u0 = n >= kW ? kItem + (long long)n * warp / kW : kItem + min(warp, n);
+        u1 = n >= kW ? kItem + (long long)n * (warp + 1) / kW : kItem + min(warp + 1, n);
     } else {
-        long long base = 0;
-        for (int i0 = 0; i0 < a.n; i0 += kT) {
-            const int i = i0 + (int)threadIdx.x;
-            const long long x = i < a.n ? (long long)units_of(length(i)) * n_heads : 0;
-            long long all;
-            const long long before = base + scan(x, all);
-            if (cta0 >= before && cta0 < before + x) {
-                s_found[0] = i;
-                s_found[1] = before;
+        if ((int)blockIdx.x * kW >= workers || U == 0) return;
+        auto share = [&](int w) { return w >= workers ? U : codes::divide(U * w, workers); };
+        const int me = (int)blockIdx.x * kW + warp;
+        const long long cta0 = share((int)blockIdx.x * kW);
+        if (a.n <= kT) {
+            if (cta0 >= before_mine && cta0 < before_mine + mine * n_heads) {
+                s_found[0] = threadIdx.x;
+                s_found[1] = before_mine;
             }
-            base += all;
-            if (cta0 < base) break;
+        } else {
+            long long base = 0;
+            for (int i0 = 0; i0 < a.n; i0 += kT) {
+                const int i = i0 + (int)threadIdx.x;
+                const long long x = i < a.n ? (long long)units_of(length(i)) * n_heads : 0;
+                long long all;
+                const long long before = base + scan(x, all);
+                if (cta0 >= before && cta0 < before + x) {
+                    s_found[0] = i;
+                    s_found[1] = before;
+                }
+                base += all;
+                if (cta0 < base) break;
+            }
         }
+        __syncthreads();
+        u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
+        seq = (int)s_found[0];
+        seq0 = s_found[1];
     }
-    __syncthreads();
 
     // ---- this warp's pieces
-    const long long u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
-    int seq = (int)s_found[0];
-    long long seq0 = s_found[1];  // first unit of the sequence
     for (long long u = u0; u < u1;) {
         const int len = length(seq), n_pairs = pairs_of(len), per = units_of(len);
         if (u >= seq0 + (long long)per * n_heads) {
@@ -404,9 +424,11 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             const uint8_t* p1 = from(page.y, 2 * r + 1) - kRec;
             const uint32_t to = ptx::smem_u32(ring) + st * 2 * kRec + lane * 16;
 #pragma unroll
-            for (int k = 0; k < (2 * kRec + 511) / 512; ++k) {
-                const bool second = 512 * k + 16 * lane >= kRec;
-                if ((!second || both) && 512 * k + 16 * lane < 2 * kRec) ptx::async_copy16(to + 512 * k, (second ? p1 : p0) + 512 * k);
+            for (int k = 0; k < (2 * kRec + 511) / 512; ++k) {  // which record: known but for the lanes where they meet
+                const int at = 512 * k + 16 * lane;
+                const bool second = 512 * k >= kRec || (512 * k + 512 > kRec && at >= kRec);
+                const bool inside = 512 * k + 512 <= 2 * kRec || at < 2 * kRec;
+                if ((!second || both) && inside) ptx::async_copy16(to + 512 * k, (second ? p1 : p0) + 512 * k);
             }
         };
         int next = r0;  // pair to ask for
@@ -622,7 +644,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             else
                 s_last[warp] = 1;
             // this CTA's items that other CTAs have too
-            const int first = worker_of(item0 + kItem) / kW, last = worker_of(item0 + kItem + n_pairs - 1) / kW;
+            const int first = whole_items ? 0 : worker_of(item0 + kItem) / kW;
+            const int last = whole_items ? 0 : worker_of(item0 + kItem + n_pairs - 1) / kW;
             if (first < last) {
                 int* it = s_item[first < (int)blockIdx.x ? 0 : 1];
                 it[0] = seq, it[1] = hb, it[2] = first, it[3] = last - first + 1;

@@ -75,6 +75,7 @@ struct Piece {
 };
 constexpr int kPieces = 4;
 constexpr int kItem = 5;
+constexpr int kSplit = 12;  // units that writing and adding partial results takes as long as
 
 struct Shape {
     const CacheView& c;
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __shared__ uint64_t pc_full[kPieces], pc_empty[kPieces];
     __shared__ Piece ring[kPieces];
     __shared__ uint32_t tmem_base_sh;
-    __shared__ int abort_flag, s_last;
+    __shared__ int abort_flag, s_last, s_most;
     __shared__ long long s_scan[kThreads / 32], s_found[2];
     __shared__ long long s_units[2];  // all units; this CTA's first
     __shared__ int s_begin[3];  // the item that the share begins in: key head, block, its first unit from the share's
@@ -131,6 +132,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         abort_flag = 0;
+        s_most = 0;
         ptx::mbar_init(&q_full, 8);
         for (int s = 0; s < kK; ++s) {
             ptx::mbar_init(&k_full[s], 2);
@@ -203,13 +205,26 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const int len = shape.length(i);
         none |= shape.steps(len, 0) == 0;
         mine += shape.head_units(len);
+        atomicMax(&s_most, shape.steps(len, shape.blocks - 1) * shape.tiles(0));
     }
     const long long before_mine = scan(mine, U) * c.Hk;
     U *= c.Hk;
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
-    const bool idle = (int)blockIdx.x >= G || U == 0;
-    const long long u0 = idle ? 0 : codes::divide(U * blockIdx.x, G), u1 = idle ? 0 : codes::divide(U * (blockIdx.x + 1), G);
-    if (a.n <= kThreads) {
+    bool idle = (int)blockIdx.x >= G || U == 0;
+    long long u0 = idle ? 0 : codes::divide(U * blockIdx.x, G), u1 = idle ? 0 : codes::divide(U * (blockIdx.x + 1), G);
+    // Few items: one for a CTA, if the longest is done before an even split and its merge.
+    const long long items = (long long)a.n * c.Hk * shape.blocks;
+    const bool whole_items = items <= gridDim.x && s_most <= codes::divide(U, gridDim.x) + kSplit;
+    if (whole_items) {
+        const int x = (int)blockIdx.x, blk = x % shape.blocks, i = x / shape.blocks / c.Hk;
+        idle = x >= items;
+        u0 = 0, u1 = idle ? 0 : shape.units(shape.length(i), blk);
+        idle |= u1 == 0;
+        if (threadIdx.x == 0) {
+            s_found[0] = i;
+            s_begin[0] = x / shape.blocks % c.Hk, s_begin[1] = blk, s_begin[2] = 0;
+        }
+    } else if (a.n <= kThreads) {
         if (!idle && u0 >= before_mine && u0 < before_mine + mine * c.Hk) {
             s_found[0] = threadIdx.x;
             s_found[1] = before_mine;
@@ -235,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     }
     none = __syncthreads_or(none);
     // The block that the share begins in, where a head's blocks are no more than the threads.
-    if (!idle && shape.blocks <= kThreads) {
+    if (!idle && !whole_items && shape.blocks <= kThreads) {
         const int len = shape.length((int)s_found[0]);
         long long per;
         const long long before = scan((int)threadIdx.x < shape.blocks ? shape.units(len, threadIdx.x) : 0, per);
@@ -272,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (end > 0) {
                     seq = (int)s_found[0];
                     len = shape.length(seq);
-                    if (shape.blocks <= kThreads) {
+                    if (whole_items || shape.blocks <= kThreads) {
                         hk = s_begin[0], blk = s_begin[1], at = s_begin[2];
                     } else {
                         const long long per = shape.head_units(len);
