@@ -20,6 +20,10 @@
 //   warps 8-11  softmax of tile 0, warps 12-15 of tile 1: a thread per row. They
 //               also put Q into shared memory, as f16 with the row's largest value
 //               near 2^14 (the row's power of two joins the softmax scale)
+// An item of one tile has both softmax warpgroups take its steps in turn (even and
+// odd ones), each with scores, maximum, sum and output of its own; the first adds
+// the two at the end. (With one of them a step is a chain of softmax, P V and the
+// next scores: @@.)
 // TMEM columns: S0 [0,128) S1 [128,256) O0 [256,256+D) O1 [384,384+D).
 // P is written as f16 over S. The issuer puts S_t of the next step right after
 // O_t of this one, so the commit that says S_t is ready covers both, and a softmax
@@ -124,6 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __shared__ uint64_t pc_full[kPieces], pc_empty[kPieces];
     __shared__ Piece ring[kPieces];
     __shared__ uint32_t tmem_base_sh;
+    __shared__ float2 s_odd[kTile];  // of an item of one tile: maximum and sum over its odd steps
     __shared__ int abort_flag, s_last, s_most;
     __shared__ long long s_scan[kThreads / 32], s_found[2];
     __shared__ long long s_units[2];  // all units; this CTA's first
@@ -395,8 +400,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const bool r = ptx::mbar_wait_bounded(bar, parity, abort_p, wait_limit);
                 return __all_sync(0xffffffffu, r);
             };
-            auto issue_s = [&](int t, int st) {  // S_t = Q_t K^T
-                const uint64_t kd = k_desc + (uint64_t)st * kTileDesc, qd = q_desc + (uint64_t)t * kTileDesc;
+            auto issue_s = [&](int t, int st, int qt) {  // S_t = Q_qt K^T
+                const uint64_t kd = k_desc + (uint64_t)st * kTileDesc, qd = q_desc + (uint64_t)qt * kTileDesc;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint64_t off = (uint64_t)(((kk / 4) * (kTile * 128) + (kk % 4) * 32) >> 4);
@@ -422,50 +427,80 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (!ok) break;
                 ptx::tc_fence_after();
                 if (ptx::elect_one_sync()) {
-                    issue_s(0, st);
-                    if (two) issue_s(1, st);
+                    issue_s(0, st, 0);
+                    if (two) issue_s(1, st, 1);
                     ptx::mma_commit(&k_empty[st]);
                 }
                 __syncwarp();
-                for (int j = 0; j < n; ++j) {
-                    const bool more = j + 1 < n;
-                    const int st1 = st ^ 1;
-                    const uint32_t ph1 = st1 == 0 ? ph ^ 1u : ph;
-                    // V of this step, K of the next and P0 of this: probed together
-                    {
-                        const bool rv = ptx::mbar_try_wait(&v_full[st], ph);
-                        const bool rk = !more || ptx::mbar_try_wait(&k_full[st1], ph1);
-                        const bool rp = ptx::mbar_try_wait(&p_full[0], p_ph0);
-                        if (!__all_sync(0xffffffffu, rv && rk && rp))
-                            ok = wait_all(&v_full[st], ph) && (!more || wait_all(&k_full[st1], ph1)) && wait_all(&p_full[0], p_ph0);
-                    }
-                    if (!ok) break;
-                    p_ph0 ^= 1u;
-                    ptx::tc_fence_after();
-                    if (ptx::elect_one_sync()) {
-                        issue_o(0, st, j > 0);
-                        if (more) issue_s(0, st1);
-                        if (!two) {
-                            ptx::mma_commit(&v_empty[st]);
-                            if (more) ptx::mma_commit(&k_empty[st1]);
+                if (two) {
+                    for (int j = 0; j < n; ++j) {
+                        const bool more = j + 1 < n;
+                        const int st1 = st ^ 1;
+                        const uint32_t ph1 = st1 == 0 ? ph ^ 1u : ph;
+                        // V of this step, K of the next and P0 of this: probed together
+                        {
+                            const bool rv = ptx::mbar_try_wait(&v_full[st], ph);
+                            const bool rk = !more || ptx::mbar_try_wait(&k_full[st1], ph1);
+                            const bool rp = ptx::mbar_try_wait(&p_full[0], p_ph0);
+                            if (!__all_sync(0xffffffffu, rv && rk && rp))
+                                ok = wait_all(&v_full[st], ph) && (!more || wait_all(&k_full[st1], ph1)) && wait_all(&p_full[0], p_ph0);
                         }
-                    }
-                    __syncwarp();
-                    if (two) {
+                        if (!ok) break;
+                        p_ph0 ^= 1u;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one_sync()) {
+                            issue_o(0, st, j > 0);
+                            if (more) issue_s(0, st1, 0);
+                        }
+                        __syncwarp();
                         ok = wait_all(&p_full[1], p_ph1);
                         if (!ok) break;
                         p_ph1 ^= 1u;
                         ptx::tc_fence_after();
                         if (ptx::elect_one_sync()) {
                             issue_o(1, st, j > 0);
-                            if (more) issue_s(1, st1);
+                            if (more) issue_s(1, st1, 1);
                             ptx::mma_commit(&v_empty[st]);
                             if (more) ptx::mma_commit(&k_empty[st1]);
                         }
                         __syncwarp();
+                        st = st1;
+                        ph = ph1;
                     }
-                    st = st1;
-                    ph = ph1;
+                } else {
+                    // Q is the first tile's for both; K and V of step j are in slot (st + j) % 2
+                    auto scores = [&](int j) {
+                        const int sk = st ^ (j & 1);
+                        const uint32_t pk = ph ^ (uint32_t)((st + j) >> 1 & 1);
+                        if (!wait_all(&k_full[sk], pk)) return false;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one_sync()) {
+                            issue_s(j & 1, sk, 0);
+                            ptx::mma_commit(&k_empty[sk]);
+                        }
+                        __syncwarp();
+                        return true;
+                    };
+                    if (n > 1) ok = scores(1);
+                    for (int j = 0; j < n && ok; ++j) {
+                        const int t = j & 1, sv = st ^ t;
+                        const uint32_t pv = ph ^ (uint32_t)((st + j) >> 1 & 1);
+                        ok = wait_all(&v_full[sv], pv) && wait_all(&p_full[t], t ? p_ph1 : p_ph0);
+                        if (!ok) break;
+                        if (t)
+                            p_ph1 ^= 1u;
+                        else
+                            p_ph0 ^= 1u;
+                        ptx::tc_fence_after();
+                        if (ptx::elect_one_sync()) {
+                            issue_o(t, sv, j > 1);
+                            ptx::mma_commit(&v_empty[sv]);
+                        }
+                        __syncwarp();
+                        if (j + 2 < n) ok = scores(j + 2);
+                    }
+                    ph ^= (uint32_t)((st + n) >> 1 & 1);
+                    st ^= n & 1;
                 }
                 if (!ok) break;
                 if (ptx::elect_one_sync()) ptx::mma_commit(&o_full);
@@ -579,11 +614,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const uint32_t tS = tbase + t * 128 + lane_off, tO = tbase + 256 + t * 128 + lane_off;
         int ns = 0, pieces = 0;
         while (piece(pieces, pc)) {
-            const int R = pc.blk * kBlock + t * kTile + r;  // row of (sequence, key head)
-            const bool live = t * kTile + r < pc.rows;
+            const bool two = pc.tiles == 2;
+            const int br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br;  // row of the block, of (sequence, key head)
+            const bool live = br < pc.rows;
             float f = 0.f;      // to base-2 scores
             int limit = 0;      // tokens that the row sees
-            if (t < pc.tiles) {
+            {
                 // ---- Q
                 uint32_t w[D / 2];
                 if (live) {
@@ -604,23 +640,26 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const float up = codes::row_up(e2);
                 f = codes::row_factor(e2, a.scale * c.k_unit);
                 limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + a.group.div(R) : pc.len;
+                if (two || t == 0) {
 #pragma unroll
-                for (int e = 0; e < D / 8; ++e) {
-                    uint32_t y[4];
+                    for (int e = 0; e < D / 8; ++e) {
+                        uint32_t y[4];
 #pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        y[z] = codes::pack_f16(codes::bf(w[4 * e + z] & 0xffffu) * up, __uint_as_float(w[4 * e + z] & 0xffff0000u) * up);
-                    *reinterpret_cast<uint4*>(sQ + t * C::kBytes + (e / 8) * (kTile * 128) + r * 128 + (((e % 8) ^ (r & 7)) << 4)) =
-                        make_uint4(y[0], y[1], y[2], y[3]);
+                        for (int z = 0; z < 4; ++z)
+                            y[z] = codes::pack_f16(codes::bf(w[4 * e + z] & 0xffffu) * up, __uint_as_float(w[4 * e + z] & 0xffff0000u) * up);
+                        *reinterpret_cast<uint4*>(sQ + t * C::kBytes + (e / 8) * (kTile * 128) + r * 128 + (((e % 8) ^ (r & 7)) << 4)) =
+                            make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                    ptx::fence_proxy_async_smem();
                 }
-                ptx::fence_proxy_async_smem();
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&q_full);
 
             float m = kLowest, l = 0.f;
-            if (t < pc.tiles) {
-                for (int j = pc.b0; j < pc.b1; ++j, ++ns) {
+            {
+                const int first = pc.b0 + (two ? 0 : t), by = two ? 1 : 2;
+                for (int j = first; j < pc.b1; j += by, ++ns) {
                     ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&s_full[t], (uint32_t)(ns & 1), abort_p, wait_limit));
                     if (!ok) break;
                     ptx::tc_fence_after();
@@ -645,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         return fmaxf(ptx::fmax3(mx[0], mx[1], mx[2]),
                                      fmaxf(ptx::fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * f - 5.f;
                     };
-                    if (j == pc.b0) m = fmaxf(tile_max(), kLowest);
+                    if (j == first) m = fmaxf(tile_max(), kLowest);
                     uint64_t sum2[2];
                     // The maximum may lag the row's until a tile's sum passes 2^15,
                     // which f16 holds.
@@ -679,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         const float k = codes::ex2(m - m_new);
                         l *= k;
                         m = m_new;
-                        if (j > pc.b0) {
+                        if (j > first) {
 #pragma unroll 1
                             for (int e = 0; e < D / 16; ++e) {
                                 uint32_t o[16];
@@ -704,6 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     if (lane == 0) ptx::mbar_arrive(&p_full[t]);
                 }
             }
+            if (!two && t == 1 && pc.b1 - pc.b0 > 1) s_odd[r] = make_float2(m, l);
             ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
             ok = ptx::named_bar_and(1, 256, ok);
             if (!ok) break;
@@ -740,8 +780,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             };
             // A slot: [D / 4][256 rows] of four dims, then [256 rows] of maximum and sum: a warp's accesses are whole lines.
             float* slot = c.partials + (size_t)(2 * blockIdx.x + (pc.b0 > 0 ? 0 : 1)) * C::kSlot;
-            const int sr = t * kTile + r;
-            if (t < pc.tiles) {
+            const int sr = br;
+            float own = 1.f, odd = 0.f;  // weights of this warpgroup's output, and of the odd steps'
+            if (!two && t == 0 && pc.b1 - pc.b0 > 1) {
+                const float2 x = s_odd[r];
+                const float M = fmaxf(m, x.x);
+                own = codes::ex2(m - M), odd = codes::ex2(x.x - M);
+                m = M, l = own * l + odd * x.y;
+            }
+            if (two || t == 0) {
                 if (whole && live) finish(m, l);
 #pragma unroll 1
                 for (int d = 0; d < D; d += 32) {
@@ -749,6 +796,17 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ptx::tmem_ld16(tO + d, o[0]);
                     ptx::tmem_ld16(tO + d + 16, o[1]);
                     ptx::tmem_wait_ld();
+                    if (!two && pc.b1 - pc.b0 > 1) {
+                        uint32_t x[2][16];
+                        ptx::tmem_ld16(tO + 128 + d, x[0]);
+                        ptx::tmem_ld16(tO + 128 + d + 16, x[1]);
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                o[h][e] = __float_as_uint(fmaf(odd, __uint_as_float(x[h][e]), own * __uint_as_float(o[h][e])));
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (whole) {
@@ -780,7 +838,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     }
                 }
                 ptx::named_bar_sync(1, 256);
-                if (s_last && live) {
+                if (s_last && live && (two || t == 0)) {
                     auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
                     float M = kLowest, L = 0.f;
                     for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr).x);
