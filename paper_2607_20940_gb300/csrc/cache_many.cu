@@ -614,44 +614,48 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         const uint32_t tS = tbase + t * 128 + lane_off, tO = tbase + 256 + t * 128 + lane_off;
         int ns = 0, pieces = 0;
         while (piece(pieces, pc)) {
-            const bool two = pc.tiles == 2;
-            const int br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br;  // row of the block, of (sequence, key head)
-            const bool live = br < pc.rows;
-            float f = 0.f;      // to base-2 scores
-            int limit = 0;      // tokens that the row sees
+            bool two = pc.tiles == 2;
+            int br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br;  // row of the block, of (sequence, key head)
+            bool live = br < pc.rows;
+            const int limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + a.group.div(R) : pc.len;  // tokens that the row sees
+            float f;  // to base-2 scores
             {
-                // ---- Q
-                uint32_t w[D / 2];
-                if (live) {
-                    const uint16_t* q = a.q + place(a.q_st, pc.seq, pc.hk, R);
+                // ---- Q: kLanes lanes have a row, 16 bytes each. (A thread a row would
+                // ask for 32 lines an instruction: 3 to 6 us a piece.)
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kTurns = 32 / kAtOnce;
+                const long long q_at = live ? place(a.q_st, pc.seq, pc.hk, R) : -1;
+                const int part = lane % kLanes, which = lane / kLanes;
+                uint4 w[kTurns];
 #pragma unroll
-                    for (int e = 0; e < D / 8; ++e) {
-                        const uint4 y = *reinterpret_cast<const uint4*>(q + 8 * e);
-                        w[4 * e] = y.x, w[4 * e + 1] = y.y, w[4 * e + 2] = y.z, w[4 * e + 3] = y.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < D / 2; ++e) w[e] = 0u;
+                for (int i = 0; i < kTurns; ++i) {
+                    const long long at = __shfl_sync(0xffffffffu, q_at, i * kAtOnce + which);
+                    w[i] = at >= 0 ? *reinterpret_cast<const uint4*>(a.q + at + part * 8) : make_uint4(0u, 0u, 0u, 0u);
                 }
-                uint32_t top = 0;
+                int e2 = 0;
 #pragma unroll
-                for (int e = 0; e < D / 2; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
-                const int e2 = codes::row_exponent(top);
-                const float up = codes::row_up(e2);
-                f = codes::row_factor(e2, a.scale * c.k_unit);
-                limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + a.group.div(R) : pc.len;
-                if (two || t == 0) {
+                for (int i = 0; i < kTurns; ++i) {
+                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    uint32_t top = 0;
 #pragma unroll
-                    for (int e = 0; e < D / 8; ++e) {
+                    for (int z = 0; z < 4; ++z) top = __vmaxu2(top, x[z] & 0x7fff7fffu);
+#pragma unroll
+                    for (int d = 1; d < kLanes; d *= 2) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    const int e = codes::row_exponent(max(top & 0xffffu, top >> 16));
+                    const int mine = __shfl_sync(0xffffffffu, e, lane % kAtOnce * kLanes);
+                    if (lane / kAtOnce == i) e2 = mine;
+                    if (two || t == 0) {
+                        const float up = codes::row_up(e);
                         uint32_t y[4];
 #pragma unroll
                         for (int z = 0; z < 4; ++z)
-                            y[z] = codes::pack_f16(codes::bf(w[4 * e + z] & 0xffffu) * up, __uint_as_float(w[4 * e + z] & 0xffff0000u) * up);
-                        *reinterpret_cast<uint4*>(sQ + t * C::kBytes + (e / 8) * (kTile * 128) + r * 128 + (((e % 8) ^ (r & 7)) << 4)) =
+                            y[z] = codes::pack_f16(codes::bf(x[z] & 0xffffu) * up, __uint_as_float(x[z] & 0xffff0000u) * up);
+                        const int qr = wq * 32 + i * kAtOnce + which;
+                        *reinterpret_cast<uint4*>(sQ + t * C::kBytes + (part / 8) * (kTile * 128) + qr * 128 + (((part % 8) ^ (qr & 7)) << 4)) =
                             make_uint4(y[0], y[1], y[2], y[3]);
                     }
-                    ptx::fence_proxy_async_smem();
                 }
+                f = codes::row_factor(e2, a.scale * c.k_unit);
+                ptx::fence_proxy_async_smem();
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&q_full);
@@ -747,6 +751,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
             ok = ptx::named_bar_and(1, 256, ok);
             if (!ok) break;
+            // read again instead of being held over the steps, which have no register to spare
+            pc = ring[pieces % kPieces];
+            two = pc.tiles == 2, br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br, live = br < pc.rows;
             ptx::tc_fence_after();
 
             // ---- the piece's result
@@ -758,26 +765,24 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 jn = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
                 if (a.lse) a.lse[at] = jn.lse;
             };
-            auto store = [&](int d, const uint32_t (&o)[16]) {  // 16 dims of the row's result
+            // Eight dims of the row's result; base: where those of the base's row are staged.
+            auto store8 = [&](int d, const uint32_t* o, const unsigned char* base) {
+                float y[8];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float y[8];
+                for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[z]) * jn.own;
+                if (jn.other != 0.f) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(base);
+                    const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[8 * e + z]) * jn.own;
-                    const long long at = out_at + d + 8 * e;
-                    if (jn.other != 0.f) {
-                        const uint4 b = *reinterpret_cast<const uint4*>(a.base_out + at);
-                        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            y[2 * z] += jn.other * codes::bf(bw[z] & 0xffffu);
-                            y[2 * z + 1] += jn.other * __uint_as_float(bw[z] & 0xffff0000u);
-                        }
+                    for (int z = 0; z < 4; ++z) {
+                        y[2 * z] += jn.other * codes::bf(bw[z] & 0xffffu);
+                        y[2 * z + 1] += jn.other * __uint_as_float(bw[z] & 0xffff0000u);
                     }
-                    *reinterpret_cast<uint4*>(a.out + at) = make_uint4(ptx::pack_bf16(y[0], y[1]), ptx::pack_bf16(y[2], y[3]),
-                                                                       ptx::pack_bf16(y[4], y[5]), ptx::pack_bf16(y[6], y[7]));
                 }
+                *reinterpret_cast<uint4*>(a.out + out_at + d) =
+                    make_uint4(ptx::pack_bf16(y[0], y[1]), ptx::pack_bf16(y[2], y[3]), ptx::pack_bf16(y[4], y[5]), ptx::pack_bf16(y[6], y[7]));
             };
+            unsigned char* const own_q = sQ + t * C::kBytes;  // Q's space: its products are done
             // A slot: [D / 4][256 rows] of four dims, then [256 rows] of maximum and sum: a warp's accesses are whole lines.
             float* slot = c.partials + (size_t)(2 * blockIdx.x + (pc.b0 > 0 ? 0 : 1)) * C::kSlot;
             const int sr = br;
@@ -789,7 +794,28 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 m = M, l = own * l + odd * x.y;
             }
             if (two || t == 0) {
+                // Place of the row's 16 bytes of dims d .. d + 7, as Q's
+                auto staged_at = [&](int row, int d) {
+                    return own_q + (d / 64) * (kTile * 128) + row * 128 + (((d / 8 % 8) ^ (row & 7)) << 4);
+                };
+                if (whole && a.base_out) {
+                    // the warp's rows of the base, kLanes lanes a row
+                    constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+                    const long long b_at = live ? out_at : -1;
+#pragma unroll 4
+                    for (int i = 0; i < 32 / kAtOnce; ++i) {
+                        const long long at = __shfl_sync(0xffffffffu, b_at, i * kAtOnce + lane / kLanes);
+                        if (at >= 0)
+                            ptx::async_copy16(ptx::smem_u32(staged_at(wq * 32 + i * kAtOnce + lane / kLanes, lane % kLanes * 8)),
+                                              a.base_out + at + lane % kLanes * 8);
+                    }
+                    ptx::async_commit();
+                }
                 if (whole && live) finish(m, l);
+                if (whole && a.base_out) {
+                    ptx::async_wait<0>();
+                    __syncwarp();
+                }
 #pragma unroll 1
                 for (int d = 0; d < D; d += 32) {
                     uint32_t o[2][16];
@@ -810,7 +836,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (whole) {
-                            if (live) store(d + 16 * h, o[h]);
+                            if (live) {
+                                store8(d + 16 * h, o[h], staged_at(r, d + 16 * h));
+                                store8(d + 16 * h + 8, o[h] + 8, staged_at(r, d + 16 * h + 8));
+                            }
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
@@ -838,47 +867,90 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     }
                 }
                 ptx::named_bar_sync(1, 256);
-                if (s_last && live && (two || t == 0)) {
+                if (s_last && (two || t == 0)) {
                     auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
-                    float M = kLowest, L = 0.f;
-                    for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr).x);
-                    for (int k = 0; k < n; ++k) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr);
+                    auto ml_of = [&](int k) { return __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr); };
+                    // the first kHeld pieces' weights stay in registers
+                    constexpr int kHeld = 6;
+                    float M = kLowest, L = 0.f, held[kHeld], sums[kHeld];
+#pragma unroll
+                    for (int k = 0; k < kHeld; ++k) {
+                        const float2 ml = ml_of(min(k, n - 1));
+                        held[k] = k < n ? ml.x : kLowest;
+                        sums[k] = k < n ? ml.y : 0.f;
+                        M = fmaxf(M, held[k]);
+                    }
+                    for (int k = kHeld; k < n; ++k) M = fmaxf(M, ml_of(k).x);
+#pragma unroll
+                    for (int k = 0; k < kHeld; ++k) {
+                        held[k] = codes::ex2(held[k] - M);
+                        L += held[k] * sums[k];
+                    }
+                    for (int k = kHeld; k < n; ++k) {
+                        const float2 ml = ml_of(k);
                         L += codes::ex2(ml.x - M) * ml.y;
                     }
-                    finish(M, L);
-#pragma unroll 1
-                    for (int d = 0; d < D; d += 16) {
-                        uint32_t o[16];
+                    auto weight = [&](int k) {
+                        if (k >= kHeld) return codes::ex2(ml_of(k).x - M);
+                        float w = held[0];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = 0u;
-                        // kTogether pieces' loads at a time: each round trip costs half a microsecond
-                        constexpr int kTogether = 4;
-#pragma unroll 1
-                        for (int k = 0; k < n; k += kTogether) {
-                            float4 y[kTogether][4];
-                            float w[kTogether];
+                        for (int z = 1; z < kHeld; ++z) w = k == z ? held[z] : w;
+                        return w;
+                    };
+                    if (live) finish(M, L);
+                    // kDims dims of a piece at a time, and after a step's pieces those of
+                    // the base, through Q's space: every thread copies and reads its own
+                    // row, kDepth ahead.
+                    constexpr int kDims = D / 8, kDepth = 3, kStage = kTile * kDims * 4, kBase = kTile * kDims * 2;
+                    static_assert(kDepth * kStage + 2 * kBase <= C::kBytes, "the ring fits Q's space");
+                    const uint32_t to = ptx::smem_u32(own_q) + r * 16;
+                    int ask_k = 0, ask_d = 0;
+                    auto ask = [&](int slot_no) {
+                        if (ask_d < D) {
+                            const float4* from = reinterpret_cast<const float4*>(slot_of(ask_k)) + (ask_d / 4) * kBlock + sr;
 #pragma unroll
-                            for (int z = 0; z < kTogether; ++z) {
-                                const float* from = slot_of(min(k + z, n - 1));
-                                w[z] = __ldcg(reinterpret_cast<const float2*>(from + kBlock * D) + sr).x;
+                            for (int e = 0; e < kDims / 4; ++e) ptx::async_copy16(to + slot_no * kStage + e * (kTile * 16), from + e * kBlock);
+                            if (++ask_k == n) {
+                                if (a.base_out && live)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) y[z][e] = __ldcg(reinterpret_cast<const float4*>(from) + (d / 4 + e) * kBlock + sr);
-                            }
-#pragma unroll
-                            for (int z = 0; z < kTogether; ++z) {
-                                const float f = k + z < n ? codes::ex2(w[z] - M) : 0.f;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    o[4 * e] = __float_as_uint(fmaf(f, y[z][e].x, __uint_as_float(o[4 * e])));
-                                    o[4 * e + 1] = __float_as_uint(fmaf(f, y[z][e].y, __uint_as_float(o[4 * e + 1])));
-                                    o[4 * e + 2] = __float_as_uint(fmaf(f, y[z][e].z, __uint_as_float(o[4 * e + 2])));
-                                    o[4 * e + 3] = __float_as_uint(fmaf(f, y[z][e].w, __uint_as_float(o[4 * e + 3])));
-                                }
+                                    for (int e = 0; e < kDims / 8; ++e)
+                                        ptx::async_copy16(to + kDepth * kStage + (ask_d / kDims & 1) * kBase + e * (kTile * 16),
+                                                          a.base_out + out_at + ask_d + 8 * e);
+                                ask_k = 0, ask_d += kDims;
                             }
                         }
-                        store(d, o);
+                        ptx::async_commit();
+                    };
+                    for (int i = 0; i < kDepth; ++i) ask(i);
+                    int slot_no = 0;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += kDims) {
+                        uint32_t o[kDims];
+#pragma unroll
+                        for (int e = 0; e < kDims; ++e) o[e] = 0u;
+#pragma unroll 1
+                        for (int k = 0; k < n; ++k) {
+                            const float w = weight(k);
+                            ptx::async_wait<kDepth - 1>();
+#pragma unroll
+                            for (int e = 0; e < kDims / 4; ++e) {
+                                const float4 y = *reinterpret_cast<const float4*>(own_q + slot_no * kStage + e * (kTile * 16) + r * 16);
+                                o[4 * e] = __float_as_uint(fmaf(w, y.x, __uint_as_float(o[4 * e])));
+                                o[4 * e + 1] = __float_as_uint(fmaf(w, y.y, __uint_as_float(o[4 * e + 1])));
+                                o[4 * e + 2] = __float_as_uint(fmaf(w, y.z, __uint_as_float(o[4 * e + 2])));
+                                o[4 * e + 3] = __float_as_uint(fmaf(w, y.w, __uint_as_float(o[4 * e + 3])));
+                            }
+                            // the step's base came with its last piece, and is used below before its place is asked for again
+                            if (k == n - 1 && live)
+#pragma unroll
+                                for (int e = 0; e < kDims / 8; ++e)
+                                    store8(d + 8 * e, o + 8 * e, own_q + kDepth * kStage + (d / kDims & 1) * kBase + e * (kTile * 16) + r * 16);
+                            ask(slot_no);
+                            slot_no = slot_no + 1 == kDepth ? 0 : slot_no + 1;
+                        }
                     }
+                    // the next piece's Q goes where other threads' rows were
+                    ptx::named_bar_sync(2 + t, kTile);
                 }
             }
             done(pieces);
