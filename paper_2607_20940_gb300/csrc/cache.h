@@ -52,7 +52,6 @@ struct CacheView {
     int* refs;       // [pages]
     unsigned* used;  // [ceil(pages / 32)] bit p % 32 of word p / 32: refs[p] > 0
     // workspace: lists of one call
-    int* claim;      // [S]
     int* row;        // [S] first new page of a list's row (grow: times 2, plus 1 if its first is a copied last page)
     int* new_len;    // [S]
     int* free_list;  // [pages]

@@ -98,7 +98,7 @@ extern "C" msf_status msf_cache_create(const msf_cache_desc* desc, msf_cache_t* 
     i.table_offset = i.lengths_offset + round256((size_t)v.S * 4);
     i.refs_offset = i.table_offset + round256((size_t)v.S * v.W * 4);
     i.state_bytes = i.refs_offset + round256((size_t)v.pages * 4) + round256((size_t)(v.pages + 31) / 32 * 4);
-    i.workspace_bytes = 3 * round256((size_t)v.S * 4) + 2 * round256((size_t)v.pages * 4) + round256((size_t)v.pages * 8) +
+    i.workspace_bytes = 2 * round256((size_t)v.S * 4) + 2 * round256((size_t)v.pages * 4) + round256((size_t)v.pages * 8) +
                         round256((size_t)v.S * v.W * 4) + round256(msf::kCacheMaxCtas * 4) +
                         round256(msf::kCachePartialFloats * 4);
     *out = c;
@@ -135,7 +135,6 @@ extern "C" msf_status msf_cache_bind(msf_cache_t cache, void* pool, size_t pool_
         w += round256(bytes);
         return p;
     };
-    v.claim = (int*)take((size_t)v.S * 4);
     v.row = (int*)take((size_t)v.S * 4);
     v.new_len = (int*)take((size_t)v.S * 4);
     v.free_list = (int*)take((size_t)v.pages * 4);

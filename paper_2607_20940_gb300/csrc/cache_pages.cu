@@ -51,6 +51,17 @@ __device__ __forceinline__ int block_scan(int x, int* sh, int& total) {
 
 __device__ __forceinline__ int seq_of(const int* seqs, int i) { return seqs ? seqs[i] : i; }
 
+// Whether a list names a sequence twice: a bit each, in shared memory. clear_seen
+// before (with a barrier behind it); first_seen is false from the second time on.
+constexpr int kSeenWords = 65536 / 32;
+__device__ __forceinline__ void clear_seen(const CacheView& c, unsigned* seen) {
+    for (int w = threadIdx.x; w < (c.S + 31) / 32; w += kThreads) seen[w] = 0u;
+}
+__device__ __forceinline__ bool first_seen(unsigned* seen, int s) {
+    const unsigned bit = 1u << s % 32;
+    return !(atomicOr(seen + s / 32, bit) & bit);
+}
+
 // Bits of word w that stand for pages.
 __device__ __forceinline__ unsigned page_bits(const CacheView& c, int w) {
     const int n = c.pages - 32 * w;
@@ -103,6 +114,9 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
                                                               int tokens, int n) {
     __shared__ int sh[32];
     __shared__ int n_copies;
+    __shared__ unsigned seen[kSeenWords];
+    clear_seen(c, seen);
+    __syncthreads();
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
     const unsigned stop = __ldcg(c.head + kCacheStatus) & kCacheStop;
@@ -112,25 +126,16 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
     }
     if (stop) return;
     unsigned bad = 0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int s = seq_of(seqs, i);
-        if ((unsigned)s >= (unsigned)c.S)
-            bad |= kDevIndex;
-        else
-            c.claim[s] = i;
-    }
-    if (__syncthreads_or((int)bad)) {
-        if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevIndex);
-        return;
-    }
     // Pages that each row needs, and the first of them in the list of free pages.
     long long want = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         const int i = i0 + (int)threadIdx.x;
         int need = 0, copied = 0;
         if (i < n) {
-            const int s = seq_of(seqs, i), count = counts ? counts[i] : tokens, len = c.lengths[s];
-            if (c.claim[s] != i || count < 0) bad |= kDevIndex;
+            const int s = seq_of(seqs, i), count = counts ? counts[i] : tokens;
+            const bool fine = (unsigned)s < (unsigned)c.S && count >= 0 && first_seen(seen, s);
+            const int len = fine ? c.lengths[s] : 0;
+            if (!fine) bad |= kDevIndex;
             else if (count > c.W * c.P - len) bad |= kDevPages;
             else if (count > 0) {
                 if (len % c.P) {
@@ -146,7 +151,7 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
         else if (i < n) c.row[i] = 2 * ((int)want + before) + copied;
         if (want <= c.pages) want += total;
     }
-    // (barriers: the rows' places and the claims are in place)
+    // (a barrier: the rows' places are in place)
     if (bad) atomicOr(c.head + kCacheStatus, bad);
     if (__syncthreads_or((int)bad)) return;
     if (!find_free(c, (int)want, sh)) {
@@ -181,60 +186,63 @@ __global__ void __launch_bounds__(kThreads) cache_grow_kernel(const CacheView c,
 
 // ------------------------------------------------------ forking and truncating
 
-// Checks a list on one cluster: rows in [0, n), dst names within the cache and
-// once each. Writes c.new_len[i] (of source src[i], or of dst[i] itself) and
-// returns true if every CTA may go on.
+// Checks a list: rows that name sequences, dst each at most once. Every CTA of a
+// cluster does it for itself, so all come to the same answer without waiting for
+// one another; the first raises the error. Writes c.new_len[i] (of source src[i],
+// or of dst[i] itself): the same from every CTA.
 __device__ bool list_check(const CacheView& c, const int* src, const int* dst, const int* lengths, int keep_all, int n,
-                           int t, int T) {
+                           unsigned* seen) {
+    clear_seen(c, seen);
+    __syncthreads();
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
     const unsigned stop = __ldcg(c.head + kCacheStatus) & kCacheStop;
-    if (t == 0) c.head[kCacheCopies] = 0;
-    if (stop) return false;  // the same for every thread: the word does not change before the first barrier
-    for (int i = t; i < n; i += T) {
-        const int d = seq_of(dst, i);
-        if ((unsigned)d < (unsigned)c.S) c.claim[d] = i;
-    }
-    ptx::cluster_sync();
     bool bad = false;
-    for (int i = t; i < n; i += T) {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
         const int d = seq_of(dst, i), s = src ? src[i] : d;
         const int keep = lengths ? lengths[i] : keep_all;
-        if ((unsigned)d >= (unsigned)c.S || (unsigned)s >= (unsigned)c.S || keep < 0 || __ldcg(c.claim + d) != i)
+        if ((unsigned)d >= (unsigned)c.S || (unsigned)s >= (unsigned)c.S || keep < 0 || !first_seen(seen, d))
             bad = true;
         else
-            c.new_len[i] = min(__ldcg(c.lengths + s), keep);
+            c.new_len[i] = min(c.lengths[s], keep);
     }
-    if (bad) atomicOr(c.head + kCacheStatus, kDevIndex);
-    ptx::cluster_sync();
-    return !(__ldcg(c.head + kCacheStatus) & kCacheStop);  // raised by this call: it was clear before
+    bad = __syncthreads_or(bad);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        c.head[kCacheCopies] = 0;
+        if (bad && !stop) atomicOr(c.head + kCacheStatus, kDevIndex);
+    }
+    return !bad && !stop;  // stop may be this call's, raised by its first CTA: then this one finds the same
 }
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     cache_fork_kernel(const CacheView c, const int* src, const int* dst, const int* lengths, int n, int copy) {
     __shared__ int sh[32];
-    ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
+    __shared__ unsigned seen[kSeenWords];
     const int t = (int)blockIdx.x * kThreads + (int)threadIdx.x, T = kCluster * kThreads;
-    if (!list_check(c, src, dst, lengths, 0x7fffffff, n, t, T)) return;
+    if (!list_check(c, src, dst, lengths, 0x7fffffff, n, seen)) return;
     if (copy) {
         if (blockIdx.x == 0) {
             long long want = 0;
             for (int i0 = 0; i0 < n; i0 += kThreads) {
                 const int i = i0 + (int)threadIdx.x;
-                const int need = i < n ? cache_need(c, __ldcg(c.new_len + i)) : 0;
+                const int need = i < n ? cache_need(c, c.new_len[i]) : 0;
                 int total;
                 const int before = block_scan(min(need, c.pages + 1), sh, total);
                 if (i < n) c.row[i] = (int)want + before;
                 want += total;
                 if (want > c.pages) break;
             }
-            if (want > c.pages || !find_free(c, (int)want, sh)) {
-                if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevPages);
-            } else if (threadIdx.x == 0) {
-                c.head[kCacheCopies] = (unsigned)want;
+            const bool full = want > c.pages || !find_free(c, (int)want, sh);
+            if (threadIdx.x == 0) {
+                if (full || want == 0) c.free_list[0] = full ? -1 : 0;  // for the other CTAs
+                if (!full) c.head[kCacheCopies] = (unsigned)want;
             }
         }
         ptx::cluster_sync();
-        if (__ldcg(c.head + kCacheStatus) & kCacheStop) return;
+        if (__ldcg(c.free_list) < 0) {
+            if (t == 0) atomicOr(c.head + kCacheStatus, kDevPages);
+            return;
+        }
     }
     // The new rows, before any table changes. A warp takes 32 columns of a row at a time.
     const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
@@ -272,10 +280,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     cache_truncate_kernel(const CacheView c, const int* seqs, const int* lengths, int n) {
-    ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
+    __shared__ unsigned seen[kSeenWords];
     const int t = (int)blockIdx.x * kThreads + (int)threadIdx.x, T = kCluster * kThreads;
-    if (!list_check(c, nullptr, seqs, lengths, 0, n, t, T)) return;
+    if (!list_check(c, nullptr, seqs, lengths, 0, n, seen)) return;
+    ptx::cluster_sync();  // lengths change from here on
     const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
     for (long long x = warp; x < (long long)n * strips; x += warps) {
         const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
