@@ -44,7 +44,8 @@ struct CacheView {
     int L, Hk, D, P, pages, S, W;
     int log2_p;
     long long page_bytes;
-    float k_unit, v_unit;  // 2^exponent
+    float k_unit, v_unit;    // 2^exponent
+    float k_sixth, v_sixth;  // 1 / (6 * 2^exponent)
     // state
     unsigned* head;  // kCacheStatus...
     int* lengths;    // [S]

@@ -89,6 +89,8 @@ extern "C" msf_status msf_cache_create(const msf_cache_desc* desc, msf_cache_t* 
     v.page_bytes = (long long)v.Hk * (v.P / msf::kCacheBlock) * msf::cache_record_bytes(v.D);
     v.k_unit = ldexpf(1.f, d.k_exponent);
     v.v_unit = ldexpf(1.f, d.v_exponent);
+    v.k_sixth = ldexpf(1.f / 6.f, -d.k_exponent);
+    v.v_sixth = ldexpf(1.f / 6.f, -d.v_exponent);
 
     using msf::round256;
     msf_cache_info& i = c->info;

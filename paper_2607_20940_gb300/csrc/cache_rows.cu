@@ -2,18 +2,24 @@
 //
 // A thread takes 16 neighbours of a head (a block: one scale, eight bytes of
 // codes) of a token's key and of its value. Bound: HBM; an append reads two bytes
-// a value and writes 9/16.
+// a value and writes 9/16, a read the other way round.
 //
-// A code is the nearest of the e2m1 values to x / t, t = scale * 2^exponent, ties
-// to even. The kernel rounds x * (1 / t) to multiples of 2^-12 first, which gives
-// the same code: x has 8 significant bits and a midpoint between two values times
-// t has at most 7 (3 and 4), so x is a midpoint exactly or at least 2^-9 of it away;
-// the product is within 2^-22 of the quotient, so a midpoint is brought back to
-// itself and nothing else reaches one. (Sixteen divisions a block had bound the
-// kernel instead of HBM.)
+// A scale is the nearest e4m3 value to top / (6 * 2^exponent), ties to even, and a
+// code the nearest of the e2m1 values to x / t, t = scale * 2^exponent. Neither is
+// divided (sixteen divisions a block had bound the kernel instead of HBM):
+//   scale  top has 8 significant bits and six times a midpoint between two e4m3
+//          values at most 7, so the quotient is a midpoint exactly or at least 2^-9 of
+//          it away. The product with 1 / 6, rounded to 12 significant bits, is the
+//          same midpoint, or on the same side of it.
+//   code   x has 8 significant bits and a midpoint between two values times t at
+//          most 7 (3 and 4), so the quotient is a midpoint exactly or at least 2^-9 of it
+//          away; x * (1 / t) with an approximate reciprocal (2^-22) is within 2^-19 of
+//          it up to 8, so rounded to a multiple of 2^-12 (by adding 3072) it is
+//          the same midpoint, or on the same side.
 #include <cuda_runtime.h>
 
 #include "cache.h"
+#include "cache_codes.cuh"
 #include "internal.h"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -21,12 +27,13 @@
 namespace msf {
 namespace {
 
-// Two values to e2m1 (nearest, ties to even, saturating): the lower in the low half byte.
-__device__ __forceinline__ uint32_t to_e2m1x2(float lo, float hi) {
+// Eight values to e2m1 (nearest, ties to even, saturating), the first in the lowest half byte.
+__device__ __forceinline__ uint32_t to_e2m1x8(const float (&x)[8]) {
     uint32_t r;
-    asm("{\n.reg .b8 b;\n.reg .b16 h;\ncvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\nmov.b16 h, {b, 0};\ncvt.u32.u16 %0, h;\n}"
+    asm("{\n.reg .b8 a, b, c, d;\ncvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\ncvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\ncvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\nmov.b32 %0, {a, b, c, d};\n}"
         : "=r"(r)
-        : "f"(lo), "f"(hi));
+        : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
     return r;
 }
 __device__ __forceinline__ uint32_t to_e4m3(float x) {
@@ -34,101 +41,158 @@ __device__ __forceinline__ uint32_t to_e4m3(float x) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(x));
     return r & 0xff;
 }
-__device__ __forceinline__ float from_e4m3(uint32_t b) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)b));
-    float f;
-    asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.f32.f16 %0, l;\n}" : "=f"(f) : "r"(r));
-    return f;
-}
-// The two codes of a byte as f16.
-__device__ __forceinline__ uint32_t from_e2m1x2(uint32_t byte) {
-    uint32_t r;
-    asm("{\n.reg .b8 a, b, c, d;\nmov.b32 {a, b, c, d}, %1;\ncvt.rn.f16x2.e2m1x2 %0, a;\n}" : "=r"(r) : "r"(byte));
-    return r;
-}
 __device__ __forceinline__ float f16_lo(uint32_t x) {
     float f;
     asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.f32.f16 %0, l;\n}" : "=f"(f) : "r"(x));
     return f;
 }
 __device__ __forceinline__ float f16_hi(uint32_t x) { return f16_lo(x >> 16); }
+__device__ __forceinline__ float from_e4m3(uint32_t b) { return f16_lo(codes::e4m3_f16x2(b)); }
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Pairs of fp32 values in one instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 
-// Where block `blk` of a token's keys (which = 0) or values lies: its codes, and its scale.
-__device__ __forceinline__ void block_at(const CacheView& c, int layer, int page, int head, int in_page, int blk, int which,
-                                         uint8_t*& codes, uint8_t*& scale) {
-    const int group = in_page / kCacheBlock, t = in_page % kCacheBlock;
-    uint8_t* rec = c.pool + ((long long)layer * c.pages + page) * c.page_bytes +
-                   (long long)(head * (c.P / kCacheBlock) + group) * cache_record_bytes(c.D);
-    if (which == 0) {
-        codes = rec + t * (c.D / 2) + blk * 8;
-        scale = rec + cache_k_scales(c.D) + t * (c.D / kCacheBlock) + blk;
+// 16 bf16 values, as one access where they begin at a multiple of 32 bytes.
+__device__ __forceinline__ void load16(uint32_t (&w)[8], const uint16_t* p, bool wide) {
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
     } else {
-        codes = rec + cache_v_codes(c.D) + t * (c.D / 2) + cache_v_code_at(c.D, t, blk * 8);
-        scale = rec + cache_v_scales(c.D) + blk * kCacheBlock + cache_v_scale_at(t);
+        const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store16(uint16_t* p, const uint32_t (&w)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
     }
 }
 
-// Units: (row of the list, token, head, block); a block of threads takes kSpan
-// neighbouring ones of a row of the list.
-constexpr int kThreads = 256, kEach = 2, kSpan = kThreads * kEach;
+// Units: (row of the list, group of tokens, head, token of the group, block); a
+// block of threads takes kSpan neighbouring ones of a row of the list. A group is
+// what a warp holds of one head, so that its codes and scales are whole lines (one
+// token for calls of fewer tokens).
+constexpr int kThreads = 128, kEach = 2, kSpan = kThreads * kEach;
 
 struct UnitGrid {
-    FastDiv per_token;  // Hk * D / 16 units
-    int nb_log2;        // blocks of a head: 4 or 8
+    FastDiv per_group;  // Hk * D / 16 units, times a group's tokens
+    int group_log2;
+    bool wide;  // rows begin at multiples of 32 bytes
 };
 
-__global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheView c, const CacheRows r, const UnitGrid u,
+template <int D>
+struct Unit {
+    static constexpr int kNbLog2 = D == 128 ? 3 : 2;
+    int h, blk;
+    unsigned t;  // (past 2^31 behind the last token of a call of that many)
+    __device__ __forceinline__ Unit(const UnitGrid& u, int x, int g0) {
+        const int dg = u.per_group.div(x), y = x - dg * u.per_group.d;
+        blk = y & ((1 << kNbLog2) - 1);
+        t = ((unsigned)(g0 + dg) << u.group_log2) + ((y >> kNbLog2) & ((1 << u.group_log2) - 1));
+        h = y >> (kNbLog2 + u.group_log2);
+    }
+};
+// The record of 16 tokens of a head that `in_page` is of.
+template <int D>
+__device__ __forceinline__ uint8_t* record_at(const CacheView& c, int layer, int page, int h, int in_page) {
+    return c.pool + ((long long)layer * c.pages + page) * c.page_bytes +
+           (long long)(h * (c.P / kCacheBlock) + in_page / kCacheBlock) * cache_record_bytes(D);
+}
+// Where block `blk` of its token t has its codes and scale: of the keys (which = 0) or values.
+template <int D>
+__device__ __forceinline__ int codes_at(int t, int blk, int which) {
+    return which ? cache_v_codes(D) + t * (D / 2) + cache_v_code_at(D, t, blk * 8) : t * (D / 2) + blk * 8;
+}
+template <int D>
+__device__ __forceinline__ int scale_at(int t, int blk, int which) {
+    return which ? cache_v_scales(D) + blk * kCacheBlock + cache_v_scale_at(t) : cache_k_scales(D) + t * (D / kCacheBlock) + blk;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 8) cache_write_kernel(const CacheView c, const CacheRows r, const UnitGrid u,
                                                                const uint16_t* k, const uint16_t* v) {
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
     if (__ldcg(c.head + kCacheStatus) & kCacheStop) return;
+    const long long first = (long long)blockIdx.x * kSpan;
+    const int g0 = (int)codes::divide(first, u.per_group.d), rest = (int)(first - (long long)g0 * u.per_group.d);
     for (int i = blockIdx.y; i < r.n; i += gridDim.y) {
         const int s = r.seqs ? r.seqs[i] : i, count = r.at ? r.at[i] : r.tokens;
         if ((unsigned)s >= (unsigned)c.S || count < 0 || count > r.tokens) {
             if (threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevIndex);
             continue;
         }
-        const long long first = (long long)blockIdx.x * kSpan;
-        const int t0 = (int)(first / u.per_token.d), rest = (int)(first - (long long)t0 * u.per_token.d);
-        if (t0 >= count) continue;
-        const int pos0 = c.lengths[s] - count;
-        const int* row = c.table + (size_t)s * c.W;
-        uint4 w[kEach][2][2];
-        uint8_t *codes[kEach][2], *scale[kEach][2];
-        bool live[kEach];
+        if ((unsigned)g0 << u.group_log2 >= (unsigned)count) continue;
+        // the rows are on their way while their places are found
+        uint32_t w[kEach][2][8];
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int x = rest + e * kThreads + (int)threadIdx.x, dt = u.per_token.div(x);
-            const int t = t0 + dt, unit = x - dt * u.per_token.d, h = unit >> u.nb_log2, blk = unit & ((1 << u.nb_log2) - 1);
-            const int pos = pos0 + t;
-            live[e] = t < count && pos >= 0 && pos < c.W * c.P;
-            if (!live[e]) continue;
-            const int page = row[pos >> c.log2_p];
-            if (!cache_page_ok(c, page) || c.refs[page] > 1) {
+            const Unit<D> x(u, rest + e * kThreads + (int)threadIdx.x, g0);
+            if (x.t >= (unsigned)count) continue;
+            const long long at = i * r.st[0] + x.t * r.st[1] + x.h * r.st[2] + x.blk * kCacheBlock;
+            load16(w[e][0], k + at, u.wide);
+            load16(w[e][1], v + at, u.wide);
+        }
+        const int pos0 = c.lengths[s] - count;
+        const int* row = c.table + (size_t)s * c.W;
+        int page[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const Unit<D> x(u, rest + e * kThreads + (int)threadIdx.x, g0);
+            const int pos = pos0 + (int)x.t;
+            page[e] = -1;
+            if (x.t >= (unsigned)count || pos < 0 || pos >= c.W * c.P) continue;
+            page[e] = row[pos >> c.log2_p];
+            if (!cache_page_ok(c, page[e]) || c.refs[page[e]] > 1) {
                 atomicOr(c.head + kCacheStatus, kDevIndex);
-                live[e] = false;
-                continue;
+                page[e] = -1;
             }
-            const long long at = i * r.st[0] + t * r.st[1] + h * r.st[2] + blk * kCacheBlock;
-            w[e][0][0] = *reinterpret_cast<const uint4*>(k + at);
-            w[e][0][1] = *reinterpret_cast<const uint4*>(k + at + 8);
-            w[e][1][0] = *reinterpret_cast<const uint4*>(v + at);
-            w[e][1][1] = *reinterpret_cast<const uint4*>(v + at + 8);
-            block_at(c, r.layer, page, h, pos & (c.P - 1), blk, 0, codes[e][0], scale[e][0]);
-            block_at(c, r.layer, page, h, pos & (c.P - 1), blk, 1, codes[e][1], scale[e][1]);
         }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            if (!live[e]) continue;
+            if (page[e] < 0) continue;
+            const Unit<D> x(u, rest + e * kThreads + (int)threadIdx.x, g0);
+            const int in_page = (pos0 + (int)x.t) & (c.P - 1), t = in_page % kCacheBlock;
+            uint8_t* rec = record_at<D>(c, r.layer, page[e], x.h, in_page);
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
-                uint32_t y[8] = {w[e][which][0].x, w[e][which][0].y, w[e][which][0].z, w[e][which][0].w,
-                                 w[e][which][1].x, w[e][which][1].y, w[e][which][1].z, w[e][which][1].w};
-                uint32_t top = 0;  // largest magnitudes, as bits, of the lower and upper halves
+                uint32_t(&y)[8] = w[e][which];
+                // largest magnitudes of the lower and upper halves
+                uint32_t most = y[0];
 #pragma unroll
-                for (int z = 0; z < 8; ++z) top = __vmaxu2(top, y[z] & 0x7fff7fffu);
-                top = max(top & 0xffffu, top >> 16);
+                for (int z = 1; z < 8; ++z) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(most) : "r"(y[z]));
+                most &= 0x7fff7fffu;
+                uint32_t top = max(most & 0xffffu, most >> 16);
                 if (top >= 0x7f80u) {  // infinities or NaN
                     atomicOr(c.head + kCacheStatus, kDevNonfinite);
                     top = 0;
@@ -145,82 +209,99 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheView c
                         y[z] = h[0] | h[1] << 16;
                     }
                 }
-                const float unit = which ? c.v_unit : c.k_unit;
-                uint32_t sc = to_e4m3(__fdiv_rn(__uint_as_float(top << 16), 6.f * unit));
+                const float unit = which ? c.v_unit : c.k_unit, sixth = which ? c.v_sixth : c.k_sixth;
+                const uint32_t want = (__float_as_uint(__fmul_rn(__uint_as_float(top << 16), sixth)) + 0x800u) & ~0xfffu;
+                uint32_t sc = to_e4m3(__uint_as_float(want));
                 if (sc == 0) sc = 1;  // 2^-9
-                const float inv = __frcp_rn(from_e4m3(sc) * unit);
-                uint32_t code[2] = {0u, 0u};
+                const float inv = rcp(from_e4m3(sc) * unit);
+                const uint64_t inv2 = pair(inv, inv), up = pair(3072.f, 3072.f), down = pair(-3072.f, -3072.f);
+                uint32_t code[2];
 #pragma unroll
-                for (int z = 0; z < 8; ++z) {
-                    const float lo = __fadd_rn(__fadd_rn(__fmul_rn(__uint_as_float(y[z] << 16), inv), 3072.f), -3072.f);
-                    const float hi = __fadd_rn(__fadd_rn(__fmul_rn(__uint_as_float(y[z] & 0xffff0000u), inv), 3072.f), -3072.f);
-                    code[z / 4] |= to_e2m1x2(lo, hi) << 8 * (z % 4);
+                for (int half = 0; half < 2; ++half) {
+                    float f[8];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const uint32_t b = y[4 * half + z];
+                        unpair(add2(fma2(pair(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)), inv2, up), down),
+                               f[2 * z], f[2 * z + 1]);
+                    }
+                    code[half] = to_e2m1x8(f);
                 }
-                *reinterpret_cast<uint2*>(codes[e][which]) = make_uint2(code[0], code[1]);
-                *scale[e][which] = (uint8_t)sc;
+                *reinterpret_cast<uint2*>(rec + codes_at<D>(t, x.blk, which)) = make_uint2(code[0], code[1]);
+                rec[scale_at<D>(t, x.blk, which)] = (uint8_t)sc;
             }
         }
     }
 }
 
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheView c, const CacheRows r, const UnitGrid u,
+template <int D>
+__global__ void __launch_bounds__(kThreads, 12) cache_read_kernel(const CacheView c, const CacheRows r, const UnitGrid u,
                                                               uint16_t* k, uint16_t* v) {
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
+    const long long first = (long long)blockIdx.x * kSpan;
+    const int g0 = (int)codes::divide(first, u.per_group.d), rest = (int)(first - (long long)g0 * u.per_group.d);
     for (int i = blockIdx.y; i < r.n; i += gridDim.y) {
         const int s = r.seqs ? r.seqs[i] : i;
         const bool some = (unsigned)s < (unsigned)c.S;
         if (!some && threadIdx.x == 0) atomicOr(c.head + kCacheStatus, kDevIndex);
-        const long long first = (long long)blockIdx.x * kSpan;
-        const int t0 = (int)(first / u.per_token.d), rest = (int)(first - (long long)t0 * u.per_token.d);
         const int begin = r.at ? r.at[i] : 0, len = some ? min(c.lengths[s], c.W * c.P) : 0;
         const int* row = c.table + (size_t)(some ? s : 0) * c.W;
         uint2 q[kEach][2];
         uint32_t sc[kEach][2];
-        long long at[kEach];
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int x = rest + e * kThreads + (int)threadIdx.x, dt = u.per_token.div(x);
-            const int t = t0 + dt, unit = x - dt * u.per_token.d, h = unit >> u.nb_log2, blk = unit & ((1 << u.nb_log2) - 1);
-            at[e] = t < r.tokens ? i * r.st[0] + t * r.st[1] + h * r.st[2] + blk * kCacheBlock : -1;
-            const long long pos = (long long)begin + t;
+            const Unit<D> x(u, rest + e * kThreads + (int)threadIdx.x, g0);
+            const long long pos = (long long)begin + x.t;
             q[e][0] = q[e][1] = make_uint2(0u, 0u);
             sc[e][0] = sc[e][1] = 0u;
-            if (at[e] < 0 || pos < 0 || pos >= len) continue;
-            const int page = row[(int)pos >> c.log2_p];
-            if (!cache_page_ok(c, page)) continue;
+            if (x.t >= (unsigned)r.tokens || pos < 0 || pos >= (long long)c.W * c.P) continue;
+            const int page = row[(int)pos >> c.log2_p];  // (not held up by the length)
+            if (pos >= len || !cache_page_ok(c, page)) continue;
+            const int in_page = (int)pos & (c.P - 1), t = in_page % kCacheBlock;
+            const uint8_t* rec = record_at<D>(c, r.layer, page, x.h, in_page);
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
-                uint8_t *codes, *scale;
-                block_at(c, r.layer, page, h, (int)pos & (c.P - 1), blk, which, codes, scale);
-                q[e][which] = *reinterpret_cast<const uint2*>(codes);
-                sc[e][which] = *scale;
+                q[e][which] = *reinterpret_cast<const uint2*>(rec + codes_at<D>(t, x.blk, which));
+                sc[e][which] = rec[scale_at<D>(t, x.blk, which)];
             }
         }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            if (at[e] < 0) continue;
+            const Unit<D> x(u, rest + e * kThreads + (int)threadIdx.x, g0);
+            if (x.t >= (unsigned)r.tokens) continue;
+            const long long at = i * r.st[0] + x.t * r.st[1] + x.h * r.st[2] + x.blk * kCacheBlock;
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
                 const float step = from_e4m3(sc[e][which]) * (which ? c.v_unit : c.k_unit);
+                const uint64_t step2 = pair(step, step);
                 uint32_t w[8];
 #pragma unroll
-                for (int z = 0; z < 8; ++z) {
-                    const uint32_t h = from_e2m1x2((z < 4 ? q[e][which].x : q[e][which].y) >> 8 * (z % 4));
-                    w[z] = ptx::pack_bf16(f16_lo(h) * step, f16_hi(h) * step);
+                for (int z = 0; z < 2; ++z) {
+                    const uint32_t eight = z ? q[e][which].y : q[e][which].x;
+                    const uint32_t h[4] = {codes::e2m1_f16x2<0>(eight), codes::e2m1_f16x2<1>(eight),
+                                           codes::e2m1_f16x2<2>(eight), codes::e2m1_f16x2<3>(eight)};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        float lo, hi;
+                        unpair(mul2(pair(f16_lo(h[y]), f16_hi(h[y])), step2), lo, hi);
+                        w[4 * z + y] = ptx::pack_bf16(lo, hi);
+                    }
                 }
-                uint16_t* dst = (which ? v : k) + at[e];
-                *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4*>(dst + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                store16((which ? v : k) + at, w, u.wide);
             }
         }
     }
 }
 
-bool grid_of(const CacheView& c, const CacheRows& r, UnitGrid& u, dim3& grid) {
-    u.nb_log2 = c.D == 128 ? 3 : 2;
-    u.per_token = FastDiv(c.Hk << u.nb_log2);
-    const long long x = ((long long)r.tokens * u.per_token.d + kSpan - 1) / kSpan;
+bool grid_of(const CacheView& c, const CacheRows& r, const void* k, const void* v, UnitGrid& u, dim3& grid) {
+    const int nb_log2 = c.D == 128 ? 3 : 2;
+    u.group_log2 = 5 - nb_log2;
+    if (r.tokens < 1 << u.group_log2) u.group_log2 = 0;
+    u.per_group = FastDiv(c.Hk << (nb_log2 + u.group_log2));
+    u.wide = (((uintptr_t)k | (uintptr_t)v | (uintptr_t)(2 * (r.st[0] | r.st[1] | r.st[2]))) & 31u) == 0;
+    const long long groups = ((long long)r.tokens + (1 << u.group_log2) - 1) >> u.group_log2;
+    const long long x = (groups * u.per_group.d + kSpan - 1) / kSpan;
     if (x >= 1ll << 31) return false;
     grid = dim3((unsigned)x, (unsigned)(r.n < 65535 ? r.n : 65535));
     return true;
@@ -232,15 +313,15 @@ cudaError_t launch_cache_write(const CacheView& c, const CacheRows& r, const uin
                                cudaStream_t st) {
     UnitGrid u;
     dim3 grid;
-    if (!grid_of(c, r, u, grid)) return cudaErrorInvalidValue;
-    return launch_pdl(cache_write_kernel, grid, dim3(kThreads), 0, st, c, r, u, k, v);
+    if (!grid_of(c, r, k, v, u, grid)) return cudaErrorInvalidValue;
+    return launch_pdl(c.D == 128 ? cache_write_kernel<128> : cache_write_kernel<64>, grid, dim3(kThreads), 0, st, c, r, u, k, v);
 }
 
 cudaError_t launch_cache_read(const CacheView& c, const CacheRows& r, uint16_t* k, uint16_t* v, cudaStream_t st) {
     UnitGrid u;
     dim3 grid;
-    if (!grid_of(c, r, u, grid)) return cudaErrorInvalidValue;
-    return launch_pdl(cache_read_kernel, grid, dim3(kThreads), 0, st, c, r, u, k, v);
+    if (!grid_of(c, r, k, v, u, grid)) return cudaErrorInvalidValue;
+    return launch_pdl(c.D == 128 ? cache_read_kernel<128> : cache_read_kernel<64>, grid, dim3(kThreads), 0, st, c, r, u, k, v);
 }
 
 }  // namespace msf

@@ -416,11 +416,22 @@ def _list(t, n=None):
     """An int32 device list (or None) and its length."""
     if t is None:
         return None, n
-    if t.dtype != _get_torch().int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+    shape = t.shape
+    if t.dtype != (_torch or _get_torch()).int32 or len(shape) != 1 or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("a list is a contiguous one-dimensional int32 tensor on the device")
-    if n is not None and t.shape[0] != n:
-        raise ValueError(f"a list has {t.shape[0]} entries where {n} are wanted")
-    return t.data_ptr(), t.shape[0]
+    got = shape[0]
+    if n is not None and got != n:
+        raise ValueError(f"a list has {got} entries where {n} are wanted")
+    return t.data_ptr(), got
+
+
+def _plain(strides, shape):
+    """Strides with 0 for dimensions of one, where they may be anything."""
+    return tuple([x if n > 1 else 0 for x, n in zip(strides, shape)])
+
+
+def _alike(a, b, shape):
+    return a == b or _plain(a, shape) == _plain(b, shape)
 
 
 def _rows(t, dtype, name, shape=None):
@@ -433,8 +444,8 @@ def _rows(t, dtype, name, shape=None):
     strides = t.stride()
     if strides[-1] != 1 and got[-1] > 1 and t.numel():
         raise ValueError(f"{name}: the last dimension has to be contiguous")
-    if 1 in got:  # the stride of a dimension of one is anything
-        return tuple(x if n > 1 else 0 for x, n in zip(strides[:-1], got))
+    if 1 in got and (strides[0] | strides[1] | strides[2]) & 7:
+        return _plain(strides[:-1], got)
     return strides[:-1]
 
 
@@ -469,17 +480,21 @@ def msf_cache_grow(cache: int, seqs, counts, tokens: int, n: int, stream=None) -
     _check(_lib.msf_cache_grow(cache, seqs, counts, tokens, n, _stream(stream)), "msf_cache_grow")
 
 
-def _row_call(fn, where, cache, layer, k, v, seqs, at, stream):
-    bf16 = _get_torch().bfloat16
+def _row_call(fn, where, cache, layer, k, v, seqs, at, stream, heads=None):
+    bf16 = (_torch or _get_torch()).bfloat16
     shape = k.shape
     if len(shape) != 4:
         raise ValueError(f"{where}: k and v are [rows, tokens, kv_heads, head_dim]")
+    n, tokens, kv_heads, dim = shape
+    if heads is not None and heads != (kv_heads, dim):
+        raise ValueError(f"rows of {(kv_heads, dim)} heads, where the cache holds {heads}")
     strides = _rows(k, bf16, "k")
-    if _rows(v, bf16, "v", shape) != strides:
+    if not _alike(_rows(v, bf16, "v", shape), strides, shape):
         raise ValueError(f"{where}: k and v have the same strides")
-    n = shape[0]
-    _check(fn(cache, layer, _list(seqs, n)[0], _list(at, n)[0], n, shape[1], k.data_ptr(), v.data_ptr(),
-              _STRIDES.pack(*strides), _stream(stream)), where)
+    status = fn(cache, layer, None if seqs is None else _list(seqs, n)[0], None if at is None else _list(at, n)[0], n,
+                tokens, k.data_ptr(), v.data_ptr(), _STRIDES.pack(*strides), _stream(stream))
+    if status:
+        raise MsfError(status, where)
 
 
 def msf_cache_write(cache: int, layer: int, k, v, seqs=None, counts=None, stream=None) -> None:
@@ -654,7 +669,7 @@ class Cache:
 
     def __init__(self, desc: msf_cache_desc):
         self.desc = desc
-        self.kv_heads, self.head_dim = desc.kv_heads, desc.head_dim
+        self.heads = self.kv_heads, self.head_dim = desc.kv_heads, desc.head_dim
         self.handle = msf_cache_create(desc)
         self.info = msf_cache_query(self.handle)
         self.bound_pool = self.bound_state = self.bound_workspace = None
@@ -702,17 +717,11 @@ class Cache:
 
     def write(self, layer, k, v, seqs=None, counts=None, stream=None):
         """Quantise the newest tokens: k, v bf16 [rows, tokens, kv_heads, head_dim]."""
-        self._heads(k)
-        msf_cache_write(self.handle, layer, k, v, seqs, counts, stream)
+        _row_call(_lib.msf_cache_write, "msf_cache_write", self.handle, layer, k, v, seqs, counts, stream, self.heads)
 
     def read(self, layer, k, v, seqs=None, begins=None, stream=None):
         """Read tokens from begins[i] on (0) back into bf16 k, v."""
-        self._heads(k)
-        msf_cache_read(self.handle, layer, k, v, seqs, begins, stream)
-
-    def _heads(self, k):
-        if k.shape[-2:] != (self.kv_heads, self.head_dim):
-            raise ValueError(f"rows of {tuple(k.shape[-2:])} heads, where the cache holds {(self.kv_heads, self.head_dim)}")
+        _row_call(_lib.msf_cache_read, "msf_cache_read", self.handle, layer, k, v, seqs, begins, stream, self.heads)
 
     def fork(self, src, dst, lengths=None, copy=False, stream=None):
         """dst[i] becomes (the first lengths[i] tokens of) src[i], sharing its pages or with copies of them."""
@@ -739,14 +748,15 @@ class Cache:
         n, queries, heads, _ = shape
         bf16 = torch.bfloat16
         q_strides, strides = _rows(q, bf16, "q"), _rows(out, bf16, "out", shape)
-        if base_out is not None and base_out is not out and _rows(base_out, bf16, "base_out", shape) != strides:
+        if base_out is not None and base_out is not out and not _alike(
+                _rows(base_out, bf16, "base_out", shape), strides, shape):
             raise ValueError("base_out and out have the same strides")
         lse_strides = (0, 0)
         if lse is not None:
             lse_strides = _rows(lse, torch.float32, "lse", (n, heads, queries))
         if base_lse is not None and base_lse is not lse:
             base_strides = _rows(base_lse, torch.float32, "base_lse", (n, heads, queries))
-            if lse is not None and base_strides != lse_strides:
+            if lse is not None and not _alike(base_strides, lse_strides, base_lse.shape):
                 raise ValueError("base_lse and lse have the same strides")
             lse_strides = base_strides
         args = _ATTENTION.pack(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
