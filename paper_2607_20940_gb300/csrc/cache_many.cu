@@ -84,10 +84,11 @@ constexpr int kSplit = 12;  // units that writing and adding partial results tak
 struct Shape {
     const CacheView& c;
     const CacheAttnArgs& a;
+    const FastDiv& by_block;  // blocks of a (sequence, key head)
     int rows, blocks;
 
-    __device__ Shape(const CacheView& c_, const CacheAttnArgs& a_)
-        : c(c_), a(a_), rows(a_.group.d * a_.queries), blocks((rows + kBlock - 1) / kBlock) {}
+    __device__ Shape(const CacheView& c_, const CacheAttnArgs& a_, const FastDiv& b_)
+        : c(c_), a(a_), by_block(b_), rows(a_.group.d * a_.queries), blocks(b_.d) {}
     __device__ int length(int i) const {
         const int s = a.seqs ? a.seqs[i] : i;
         return (unsigned)s < (unsigned)c.S ? max(0, min(c.lengths[s], c.W * c.P) - a.skip) : 0;
@@ -98,22 +99,16 @@ struct Shape {
         if (a.causal) n = min(n, max(0, n - a.queries + 1 + a.group.div(b * kBlock + block_rows(b) - 1)));
         return (n + kTile - 1) / kTile;
     }
-    // Units of an item, and of a key head of a sequence of n tokens: a step of one
-    // tile, and kItem for what an item costs besides its steps.
+    // Units of an item: a step of one tile, and kItem for what it costs besides its steps.
     __device__ int units(int n, int b) const {
         const int k = steps(n, b);
         return k > 0 ? kItem + k * tiles(b) : 0;
     }
-    __device__ long long head_units(int n) const {
-        if (!a.causal) return n > 0 ? (long long)((n + kTile - 1) / kTile) * ((rows + kTile - 1) / kTile) + (long long)kItem * blocks : 0;
-        long long u = 0;
-        for (int b = 0; b < blocks; ++b) u += units(n, b);
-        return u;
-    }
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView c, const CacheAttnArgs a, long long wait_limit) {
+__global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView c, const CacheAttnArgs a, const FastDiv by_block,
+                                                                 long long wait_limit) {
     using C = ManyCfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -129,15 +124,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __shared__ Piece ring[kPieces];
     __shared__ uint32_t tmem_base_sh;
     __shared__ float2 s_odd[kTile];  // of an item of one tile: maximum and sum over its odd steps
-    __shared__ int abort_flag, s_last, s_most;
-    __shared__ long long s_scan[kThreads / 32], s_found[2];
+    __shared__ int abort_flag, s_last[2];
+    __shared__ long long s_scan[kThreads / 32];
+    __shared__ int s_most[kThreads / 32];
     __shared__ long long s_units[2];  // all units; this CTA's first
-    __shared__ int s_begin[3];  // the item that the share begins in: key head, block, its first unit from the share's
+    __shared__ int s_begin[4];  // the item that the share begins in: key head, row of the list, block, its first unit from the share's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        s_most = 0;
         ptx::mbar_init(&q_full, 8);
         for (int s = 0; s < kK; ++s) {
             ptx::mbar_init(&k_full[s], 2);
@@ -175,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
-    const Shape shape(c, a);
+    const Shape shape(c, a, by_block);
     auto place = [&](const long long* st, int i, int hk, int r) {
         const int t = a.group.div(r);
         return i * st[0] + t * st[1] + (hk * a.group.d + r - t * a.group.d) * st[2];
@@ -185,7 +180,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         return i * a.l_st[0] + (hk * a.group.d + r - t * a.group.d) * a.l_st[1] + t;
     };
 
-    // ---- this CTA's share
+    // ---- this CTA's share. The items in order: key heads, the list's rows, blocks; every
+    // key head has the same items, U1 units of them.
+    const long long items1 = (long long)a.n * shape.blocks, items = items1 * c.Hk;
+    auto units_of = [&](long long x) {
+        if (x >= items1) return 0;
+        const int i = by_block.div((int)x);
+        return shape.units(shape.length(i), (int)x - i * shape.blocks);
+    };
+    // Sum of the threads' x before this one's, and of all. Every thread calls.
     auto scan = [&](long long x, long long& all) {
         long long v = x;
 #pragma unroll
@@ -197,76 +200,71 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         __syncthreads();
         long long before = 0;
         all = 0;
+#pragma unroll
         for (int w = 0; w < kThreads / 32; ++w) {
             if (w < warp) before += s_scan[w];
             all += s_scan[w];
         }
-        __syncthreads();
         return before + v - x;
     };
-    long long U = 0, mine = 0;
-    bool none = false;  // whether a block sees no token
-    for (int i = threadIdx.x; i < a.n; i += kThreads) {
-        const int len = shape.length(i);
-        none |= shape.steps(len, 0) == 0;
-        mine += shape.head_units(len);
-        atomicMax(&s_most, shape.steps(len, shape.blocks - 1) * shape.tiles(0));
+    long long U1, mine = 0;
+    int most = 0, least = 1;  // units of the longest item; whether none is empty
+    for (long long x = threadIdx.x; x < items1; x += kThreads) {
+        const int k = units_of(x);
+        mine += k;
+        most = max(most, k);
+        least = min(least, k);
     }
-    const long long before_mine = scan(mine, U) * c.Hk;
-    U *= c.Hk;
+    most = __reduce_max_sync(0xffffffffu, most);
+    least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) s_most[warp] = least ? most : ~most;
+    long long before = scan(mine, U1);
+    bool none = false;  // whether a block sees no token
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        const int x = s_most[w];
+        none |= x < 0;
+        most = max(most, x < 0 ? ~x : x);
+    }
+    const long long U = U1 * c.Hk;
     const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
     bool idle = (int)blockIdx.x >= G || U == 0;
     long long u0 = idle ? 0 : codes::divide(U * blockIdx.x, G), u1 = idle ? 0 : codes::divide(U * (blockIdx.x + 1), G);
     // Few items: one for a CTA, if the longest is done before an even split and its merge.
-    const long long items = (long long)a.n * c.Hk * shape.blocks;
-    const bool whole_items = items <= gridDim.x && s_most <= codes::divide(U, gridDim.x) + kSplit;
+    const bool whole_items = items <= gridDim.x && most - kItem <= codes::divide(U, gridDim.x) + kSplit;
     if (whole_items) {
-        const int x = (int)blockIdx.x, blk = x % shape.blocks, i = x / shape.blocks / c.Hk;
-        idle = x >= items;
-        u0 = 0, u1 = idle ? 0 : shape.units(shape.length(i), blk);
-        idle |= u1 == 0;
-        if (threadIdx.x == 0) {
-            s_found[0] = i;
-            s_begin[0] = x / shape.blocks % c.Hk, s_begin[1] = blk, s_begin[2] = 0;
-        }
-    } else if (a.n <= kThreads) {
-        if (!idle && u0 >= before_mine && u0 < before_mine + mine * c.Hk) {
-            s_found[0] = threadIdx.x;
-            s_found[1] = before_mine;
+        idle = (int)blockIdx.x >= items;
+        if (threadIdx.x == 0 && !idle) {
+            const int hk = (int)blockIdx.x / (int)items1, x = (int)blockIdx.x - hk * (int)items1, i = by_block.div(x);
+            s_begin[0] = hk, s_begin[1] = i, s_begin[2] = x - i * shape.blocks, s_begin[3] = 0;
+            s_units[0] = 0, s_units[1] = units_of(x);
         }
     } else if (!idle) {
-        long long base = 0;
-        for (int i0 = 0; i0 < a.n; i0 += kThreads) {
-            const int i = i0 + (int)threadIdx.x;
-            const long long x = i < a.n ? shape.head_units(shape.length(i)) * c.Hk : 0;
-            long long all;
-            const long long before = base + scan(x, all);
-            if (u0 >= before && u0 < before + x) {
-                s_found[0] = i;
-                s_found[1] = before;
+        const int hk = (int)codes::divide(u0, U1);
+        const long long rest = u0 - hk * U1;
+        auto look = [&](long long x, int k, long long first) {
+            if (rest >= first && rest < first + k) {
+                const int i = by_block.div((int)x);
+                s_begin[0] = hk, s_begin[1] = i, s_begin[2] = (int)x - i * shape.blocks, s_begin[3] = (int)(first - rest);
             }
-            base += all;
-            if (u0 < base) break;
+        };
+        if (items1 <= kThreads) {
+            look(threadIdx.x, (int)mine, before);
+        } else {
+            long long base = 0;
+            for (long long x0 = 0; base <= rest; x0 += kThreads) {
+                const int k = units_of(x0 + threadIdx.x);
+                long long all;
+                __syncthreads();
+                before = scan(k, all);
+                look(x0 + threadIdx.x, k, base + before);
+                base += all;
+            }
         }
-    }
-    if (threadIdx.x == 0) {
-        s_units[0] = U;
-        s_units[1] = u0;
-    }
-    none = __syncthreads_or(none);
-    // The block that the share begins in, where a head's blocks are no more than the threads.
-    if (!idle && !whole_items && shape.blocks <= kThreads) {
-        const int len = shape.length((int)s_found[0]);
-        long long per;
-        const long long before = scan((int)threadIdx.x < shape.blocks ? shape.units(len, threadIdx.x) : 0, per);
-        const long long in = u0 - s_found[1], hk = codes::divide(in, per), rest = in - hk * per;
-        if ((int)threadIdx.x < shape.blocks && rest >= before && rest < before + shape.units(len, threadIdx.x)) {
-            s_begin[0] = (int)hk;
-            s_begin[1] = threadIdx.x;
-            s_begin[2] = (int)(before - rest);
-        }
+        if (threadIdx.x == 0) s_units[0] = U, s_units[1] = u0;
     }
     __syncthreads();
+    if (whole_items) u0 = 0, u1 = idle ? 0 : s_units[1];
 
     bool ok = true;
     // The readers' side of the ring: the n-th piece, and that a warp is done with it.
@@ -288,17 +286,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             if (lane == 0) {
                 // Units are counted from this CTA's first.
                 const int end = (int)(u1 - u0);
-                int seq = 0, hk = 0, blk = 0, len = 0, at = 0;
+                int hk = 0, seq = 0, blk = 0, len = 0, at = 0;
                 if (end > 0) {
-                    seq = (int)s_found[0];
+                    hk = s_begin[0], seq = s_begin[1], blk = s_begin[2], at = s_begin[3];
                     len = shape.length(seq);
-                    if (whole_items || shape.blocks <= kThreads) {
-                        hk = s_begin[0], blk = s_begin[1], at = s_begin[2];
-                    } else {
-                        const long long per = shape.head_units(len);
-                        hk = (int)((u0 - s_found[1]) / per);
-                        at = (int)(s_found[1] + hk * per - u0);
-                    }
                 }
                 for (int n = 0;; ++n) {
                     if (!ptx::mbar_wait_bounded(&pc_empty[n % kPieces], (uint32_t)(n / kPieces & 1) ^ 1u, abort_p, wait_limit)) {
@@ -321,11 +312,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         if (steps > 0) at += kItem + steps * w;
                         if (++blk == shape.blocks) {
                             blk = 0;
-                            if (++hk == c.Hk) {
-                                hk = 0;
-                                while (at < end && (len = shape.length(++seq)) == 0) {
-                                }
-                            }
+                            if (++seq == a.n) seq = 0, ++hk;
+                            if (at < end)  // (so there are more)
+                                while ((len = shape.length(seq)) == 0)
+                                    if (++seq == a.n) seq = 0, ++hk;
                         }
                     }
                     const bool some = p.steps > 0;
@@ -631,20 +621,27 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     const long long at = __shfl_sync(0xffffffffu, q_at, i * kAtOnce + which);
                     w[i] = at >= 0 ? *reinterpret_cast<const uint4*>(a.q + at + part * 8) : make_uint4(0u, 0u, 0u, 0u);
                 }
-                int e2 = 0;
+                // Every row's largest: kTurns = kLanes rows of kLanes lanes each change places
+                // as they are reduced, so that lane `part` ends with that of turn `part`.
+                static_assert(kTurns == kLanes, "as many rows as lanes");
+                uint32_t top[kTurns];
 #pragma unroll
-                for (int i = 0; i < kTurns; ++i) {
-                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                    uint32_t top = 0;
+                for (int i = 0; i < kTurns; ++i)
+                    top[i] = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) top = __vmaxu2(top, x[z] & 0x7fff7fffu);
+                for (int d = kLanes / 2; d >= 1; d /= 2)
 #pragma unroll
-                    for (int d = 1; d < kLanes; d *= 2) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    const int e = codes::row_exponent(max(top & 0xffffu, top >> 16));
-                    const int mine = __shfl_sync(0xffffffffu, e, lane % kAtOnce * kLanes);
-                    if (lane / kAtOnce == i) e2 = mine;
-                    if (two || t == 0) {
-                        const float up = codes::row_up(e);
+                    for (int i = 0; i < d; ++i) {
+                        const uint32_t give = part & d ? top[i] : top[i + d], keep = part & d ? top[i + d] : top[i];
+                        top[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, d));
+                    }
+                const int e = codes::row_exponent(max(top[0] & 0xffffu, top[0] >> 16));
+                const int e2 = __shfl_sync(0xffffffffu, e, lane % kAtOnce * kLanes + lane / kAtOnce);
+                if (two || t == 0) {
+#pragma unroll
+                    for (int i = 0; i < kTurns; ++i) {
+                        const float up = codes::row_up(__shfl_sync(0xffffffffu, e, which * kLanes + i));
+                        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
                         uint32_t y[4];
 #pragma unroll
                         for (int z = 0; z < 4; ++z)
@@ -748,6 +745,24 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
             }
             if (!two && t == 1 && pc.b1 - pc.b0 > 1) s_odd[r] = make_float2(m, l);
+            // An item of several CTAs: its first, and how many. The last of them to come here
+            // adds the others' results, which they leave in slots, to its own.
+            auto ctas_of = [&](const Piece& p, int& n) {
+                const long long all = s_units[0], u = s_units[1] + p.item0 + kItem;
+                const int ctas = (int)min((long long)gridDim.x, max(1ll, all / 2));
+                auto cta_of = [&](long long v) { return (int)codes::divide((v + 1) * ctas - 1, all); };
+                const int first = cta_of(u);
+                n = cta_of(u + (long long)(p.steps - 1) * p.tiles) - first + 1;
+                return first;
+            };
+            if (threadIdx.x == 256 && ok) {
+                const Piece& p = ring[pieces % kPieces];
+                if (p.b0 > 0 || p.b1 < p.steps) {
+                    int n;
+                    const int first = ctas_of(p, n);
+                    s_last[pieces & 1] = (atomicAdd(c.counters + first, 1u) & 0xffffu) == (unsigned)n - 1;
+                }
+            }
             ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
             ok = ptx::named_bar_and(1, 256, ok);
             if (!ok) break;
@@ -757,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             ptx::tc_fence_after();
 
             // ---- the piece's result
-            const bool whole = pc.b0 == 0 && pc.b1 == pc.steps;
+            const bool whole = pc.b0 == 0 && pc.b1 == pc.steps, last = !whole && s_last[pieces & 1];
             codes::Join jn;
             const long long out_at = live ? place(a.o_st, pc.seq, pc.hk, R) : 0;
             auto finish = [&](float M, float L) {
@@ -793,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 own = codes::ex2(m - M), odd = codes::ex2(x.x - M);
                 m = M, l = own * l + odd * x.y;
             }
-            if (two || t == 0) {
+            if ((two || t == 0) && !last) {
                 // Place of the row's 16 bytes of dims d .. d + 7, as Q's
                 auto staged_at = [&](int row, int d) {
                     return own_q + (d / 64) * (kTile * 128) + row * 128 + (((d / 8 % 8) ^ (row & 7)) << 4);
@@ -851,25 +866,36 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
                 if (!whole) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
             }
-            ptx::tc_fence_before();
             if (!whole) {
-                const long long all = s_units[0], u = s_units[1] + pc.item0 + kItem;
-                const int ctas = (int)min((long long)gridDim.x, max(1ll, all / 2));
-                auto cta_of = [&](long long v) { return (int)codes::divide((v + 1) * ctas - 1, all); };
-                const int first = cta_of(u), n = cta_of(u + (long long)(pc.steps - 1) * pc.tiles) - first + 1;
-                ptx::named_bar_sync(1, 256);
-                if (threadIdx.x == 256) {
-                    __threadfence();
-                    s_last = atomicAdd(c.counters + first, 1u) == (unsigned)n - 1;
-                    if (s_last) {
-                        c.counters[first] = 0;  // for the next launch
+                int n;
+                const int first = ctas_of(pc, n), me = (int)blockIdx.x - first;
+                // c.counters: pieces that came, and pieces in their slots times 2^16
+                if (!last) {
+                    ptx::named_bar_sync(1, 256);
+                    if (threadIdx.x == 256) {
+                        __threadfence();
+                        atomicAdd(c.counters + first, 1u << 16);
+                    }
+                } else {
+                    // the others have come, so they write (or have written) and wait for nothing
+                    if (threadIdx.x == 256) {
+                        const long long t0 = clock64();
+                        volatile unsigned* count = c.counters + first;
+                        while (*count >> 16 != (unsigned)n - 1 && ok) ok = clock64() - t0 < wait_limit;
+                        if (ok)
+                            *count = 0;  // for the next launch
+                        else
+                            *abort_p = 1;
                         __threadfence();
                     }
+                    ok = ptx::named_bar_and(1, 256, ok);
+                    if (!ok) break;
                 }
-                ptx::named_bar_sync(1, 256);
-                if (s_last && (two || t == 0)) {
+                if (last && (two || t == 0)) {
                     auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
-                    auto ml_of = [&](int k) { return __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr); };
+                    auto ml_of = [&](int k) {
+                        return k == me ? make_float2(m, l) : __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr);
+                    };
                     // the first kHeld pieces' weights stay in registers
                     constexpr int kHeld = 6;
                     float M = kLowest, L = 0.f, held[kHeld], sums[kHeld];
@@ -900,28 +926,31 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     if (live) finish(M, L);
                     // kDims dims of a piece at a time, and after a step's pieces those of
                     // the base, through Q's space: every thread copies and reads its own
-                    // row, kDepth ahead.
+                    // row, `depth` ahead (where a step is one copy, no more than the base has
+                    // places).
                     constexpr int kDims = D / 8, kDepth = 3, kStage = kTile * kDims * 4, kBase = kTile * kDims * 2;
                     static_assert(kDepth * kStage + 2 * kBase <= C::kBytes, "the ring fits Q's space");
+                    const int depth = n == 2 && a.base_out ? 2 : kDepth;
                     const uint32_t to = ptx::smem_u32(own_q) + r * 16;
-                    int ask_k = 0, ask_d = 0;
+                    int ask_k = me == 0 ? 1 : 0, ask_d = 0;
                     auto ask = [&](int slot_no) {
                         if (ask_d < D) {
                             const float4* from = reinterpret_cast<const float4*>(slot_of(ask_k)) + (ask_d / 4) * kBlock + sr;
 #pragma unroll
                             for (int e = 0; e < kDims / 4; ++e) ptx::async_copy16(to + slot_no * kStage + e * (kTile * 16), from + e * kBlock);
-                            if (++ask_k == n) {
+                            ask_k += ask_k + 1 == me ? 2 : 1;
+                            if (ask_k >= n) {
                                 if (a.base_out && live)
 #pragma unroll
                                     for (int e = 0; e < kDims / 8; ++e)
                                         ptx::async_copy16(to + kDepth * kStage + (ask_d / kDims & 1) * kBase + e * (kTile * 16),
                                                           a.base_out + out_at + ask_d + 8 * e);
-                                ask_k = 0, ask_d += kDims;
+                                ask_k = me == 0 ? 1 : 0, ask_d += kDims;
                             }
                         }
                         ptx::async_commit();
                     };
-                    for (int i = 0; i < kDepth; ++i) ask(i);
+                    for (int i = 0; i < depth; ++i) ask(i);
                     int slot_no = 0;
 #pragma unroll 1
                     for (int d = 0; d < D; d += kDims) {
@@ -931,28 +960,48 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 #pragma unroll 1
                         for (int k = 0; k < n; ++k) {
                             const float w = weight(k);
-                            ptx::async_wait<kDepth - 1>();
+                            float y[kDims];
+                            if (k == me) {
+                                uint32_t x[16];  // (of 64 dims, the next eight too)
+                                ptx::tmem_ld16(tO + d, x);
+                                ptx::tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < kDims / 4; ++e) {
-                                const float4 y = *reinterpret_cast<const float4*>(own_q + slot_no * kStage + e * (kTile * 16) + r * 16);
-                                o[4 * e] = __float_as_uint(fmaf(w, y.x, __uint_as_float(o[4 * e])));
-                                o[4 * e + 1] = __float_as_uint(fmaf(w, y.y, __uint_as_float(o[4 * e + 1])));
-                                o[4 * e + 2] = __float_as_uint(fmaf(w, y.z, __uint_as_float(o[4 * e + 2])));
-                                o[4 * e + 3] = __float_as_uint(fmaf(w, y.w, __uint_as_float(o[4 * e + 3])));
+                                for (int e = 0; e < kDims; ++e) y[e] = __uint_as_float(x[e]);
+                                if (!two && pc.b1 - pc.b0 > 1) {
+                                    ptx::tmem_ld16(tO + 128 + d, x);
+                                    ptx::tmem_wait_ld();
+#pragma unroll
+                                    for (int e = 0; e < kDims; ++e) y[e] = fmaf(odd, __uint_as_float(x[e]), own * y[e]);
+                                }
+                            } else {
+                                if (depth == kDepth)
+                                    ptx::async_wait<kDepth - 1>();
+                                else
+                                    ptx::async_wait<1>();
+#pragma unroll
+                                for (int e = 0; e < kDims / 4; ++e) {
+                                    const float4 z = *reinterpret_cast<const float4*>(own_q + slot_no * kStage + e * (kTile * 16) + r * 16);
+                                    y[4 * e] = z.x, y[4 * e + 1] = z.y, y[4 * e + 2] = z.z, y[4 * e + 3] = z.w;
+                                }
                             }
-                            // the step's base came with its last piece, and is used below before its place is asked for again
+#pragma unroll
+                            for (int e = 0; e < kDims; ++e) o[e] = __float_as_uint(fmaf(w, y[e], __uint_as_float(o[e])));
+                            // the step's base came with its last copy, and is used below before its place is asked for again
                             if (k == n - 1 && live)
 #pragma unroll
                                 for (int e = 0; e < kDims / 8; ++e)
                                     store8(d + 8 * e, o + 8 * e, own_q + kDepth * kStage + (d / kDims & 1) * kBase + e * (kTile * 16) + r * 16);
-                            ask(slot_no);
-                            slot_no = slot_no + 1 == kDepth ? 0 : slot_no + 1;
+                            if (k == me ? k == n - 1 : me < n - 1 || k < n - 2) {
+                                ask(slot_no);
+                                slot_no = slot_no + 1 == depth ? 0 : slot_no + 1;
+                            }
                         }
                     }
                     // the next piece's Q goes where other threads' rows were
                     ptx::named_bar_sync(2 + t, kTile);
                 }
             }
+            ptx::tc_fence_before();
             done(pieces);
             ++pieces;
         }
@@ -973,7 +1022,8 @@ cudaError_t launch_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t
     cudaError_t e = device_sms(&sms);
     if (e == cudaSuccess) e = set_smem_attr((const void*)cache_many_kernel<D>, ManyCfg<D>::kSmem, -1, kLaunchRegs);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_many_kernel<D>, dim3(sms < 160 ? sms : 160), dim3(kThreads), ManyCfg<D>::kSmem, st, c, a, kWaitLimit);
+    return launch_pdl(cache_many_kernel<D>, dim3(sms < 160 ? sms : 160), dim3(kThreads), ManyCfg<D>::kSmem, st, c, a,
+                      FastDiv((int)(((long long)a.group.d * a.queries + kBlock - 1) / kBlock)), kWaitLimit);
 }
 
 }  // namespace
