@@ -78,8 +78,9 @@ struct Piece {
     int item0;          // the item's first unit, from the CTA's first
 };
 constexpr int kPieces = 4;
-constexpr int kItem = 5;
-constexpr int kSplit = 12;  // units that writing and adding partial results takes as long as
+constexpr int kItem = 6;
+constexpr int kRowMerge = 4;  // pieces of an item of one tile up to which a thread adds a row's
+constexpr int kSplit = 16;  // units that writing and adding partial results takes as long as
 
 struct Shape {
     const CacheView& c;
@@ -773,10 +774,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
 
             // ---- the piece's result
             const bool whole = pc.b0 == 0 && pc.b1 == pc.steps, last = !whole && s_last[pieces & 1];
+            int first = 0, n = 0;
+            if (!whole) first = ctas_of(pc, n);
             codes::Join jn;
             const long long out_at = live ? place(a.o_st, pc.seq, pc.hk, R) : 0;
-            auto finish = [&](float M, float L) {
-                const long long at = lse_place(pc.seq, pc.hk, R);
+            auto finish = [&](float M, float L, int of) {
+                const long long at = lse_place(pc.seq, pc.hk, of);
                 jn = codes::join_of(M, L, a.base_lse != nullptr, a.base_lse ? a.base_lse[at] : 0.f, c.v_unit);
                 if (a.lse) a.lse[at] = jn.lse;
             };
@@ -808,7 +811,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 own = codes::ex2(m - M), odd = codes::ex2(x.x - M);
                 m = M, l = own * l + odd * x.y;
             }
-            if ((two || t == 0) && !last) {
+            const bool shared = !two && n > kRowMerge;  // both warpgroups add the pieces
+            if ((two || t == 0) && (!last || shared)) {
                 // Place of the row's 16 bytes of dims d .. d + 7, as Q's
                 auto staged_at = [&](int row, int d) {
                     return own_q + (d / 64) * (kTile * 128) + row * 128 + (((d / 8 % 8) ^ (row & 7)) << 4);
@@ -826,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     }
                     ptx::async_commit();
                 }
-                if (whole && live) finish(m, l);
+                if (whole && live) finish(m, l, R);
                 if (whole && a.base_out) {
                     ptx::async_wait<0>();
                     __syncwarp();
@@ -855,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                                 store8(d + 16 * h, o[h], staged_at(r, d + 16 * h));
                                 store8(d + 16 * h + 8, o[h] + 8, staged_at(r, d + 16 * h + 8));
                             }
-                        } else {
+                        } else if (live) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 __stcg(reinterpret_cast<float4*>(slot) + (d / 4 + 4 * h + e) * kBlock + sr,
@@ -864,11 +868,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         }
                     }
                 }
-                if (!whole) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
+                if (!whole && live) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
             }
             if (!whole) {
-                int n;
-                const int first = ctas_of(pc, n), me = (int)blockIdx.x - first;
+                const int me = (int)blockIdx.x - first;
                 // c.counters: pieces that came, and pieces in their slots times 2^16
                 if (!last) {
                     ptx::named_bar_sync(1, 256);
@@ -891,10 +894,79 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ok = ptx::named_bar_and(1, 256, ok);
                     if (!ok) break;
                 }
-                if (last && (two || t == 0)) {
-                    auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
+                auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
+                if (last && shared) {
+                    // Many pieces: all 256 threads share the rows' dims, four of a row at a time,
+                    // kDeep copies ahead through Q's space, where the weights of some rows are too.
+                    constexpr int kDeep = D == 128 ? 5 : 2, kStage = 256 * 16, kTable = (C::kBytes - kDeep * kStage - kBlock * 8) / 4;
+                    static_assert(kTable >= 160, "a row's weights fit");
+                    float *const s_own = reinterpret_cast<float*>(sQ + kDeep * kStage), *const s_other = s_own + kBlock;
+                    float* const table = s_other + kBlock;
+                    const int x = (int)threadIdx.x - 256, at_once = min(pc.rows, kTable / n);
+                    const uint32_t stage_at = ptx::smem_u32(sQ) + x * 16;
+                    __threadfence();  // this CTA's own piece is in its slot too
+                    for (int row0 = 0; row0 < pc.rows; row0 += at_once) {
+                        const int rows = min(at_once, pc.rows - row0), all = rows * (D / 4);
+                        ptx::named_bar_sync(1, 256);
+                        if (x < rows) {
+                            const int row = row0 + x;
+                            auto ml_at = [&](int k) { return __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + row); };
+                            float M = kLowest, L = 0.f;
+#pragma unroll 4
+                            for (int k = 0; k < n; ++k) M = fmaxf(M, ml_at(k).x);
+#pragma unroll 4
+                            for (int k = 0; k < n; ++k) {
+                                const float2 ml = ml_at(k);
+                                const float w = codes::ex2(ml.x - M);
+                                table[k * rows + x] = w;
+                                L += w * ml.y;
+                            }
+                            finish(M, L, pc.blk * kBlock + row);
+                            s_own[x] = jn.own, s_other[x] = jn.other;
+                        }
+                        ptx::named_bar_sync(1, 256);
+                        // element y: dims 4 (y / rows) ... of row y % rows, its place in a slot
+                        auto place_of = [&](int y) { return y / rows * (kBlock - rows) + y + row0; };
+                        int ask_y = x, ask_k = 0, ask_at = place_of(x), slot_no = 0;
+                        auto ask = [&](int to) {
+                            if (ask_y < all) {
+                                ptx::async_copy16(stage_at + to * kStage, slot_of(ask_k) + 4 * ask_at);
+                                if (++ask_k == n) {
+                                    ask_k = 0, ask_y += 256;
+                                    ask_at = place_of(ask_y);
+                                }
+                            }
+                            ptx::async_commit();
+                        };
+                        for (int i = 0; i < kDeep; ++i) ask(i);
+                        for (int y = x; y < all; y += 256) {
+                            const int d = y / rows, row = y - d * rows;
+                            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                            for (int k = 0; k < n; ++k) {
+                                ptx::async_wait<kDeep - 1>();
+                                const float w = table[k * rows + row];
+                                const float4 z = reinterpret_cast<const float4*>(sQ + slot_no * kStage)[x];
+                                acc.x = fmaf(w, z.x, acc.x), acc.y = fmaf(w, z.y, acc.y), acc.z = fmaf(w, z.z, acc.z), acc.w = fmaf(w, z.w, acc.w);
+                                ask(slot_no);
+                                slot_no = slot_no + 1 == kDeep ? 0 : slot_no + 1;
+                            }
+                            const long long at = place(a.o_st, pc.seq, pc.hk, pc.blk * kBlock + row0 + row) + 4 * d;
+                            const float ow = s_own[row], other = s_other[row];
+                            acc.x *= ow, acc.y *= ow, acc.z *= ow, acc.w *= ow;
+                            if (other != 0.f) {
+                                const uint2 b = *reinterpret_cast<const uint2*>(a.base_out + at);
+                                acc.x += other * codes::bf(b.x & 0xffffu), acc.y += other * __uint_as_float(b.x & 0xffff0000u);
+                                acc.z += other * codes::bf(b.y & 0xffffu), acc.w += other * __uint_as_float(b.y & 0xffff0000u);
+                            }
+                            *reinterpret_cast<uint2*>(a.out + at) = make_uint2(ptx::pack_bf16(acc.x, acc.y), ptx::pack_bf16(acc.z, acc.w));
+                        }
+                        ptx::async_wait<0>();
+                    }
+                    ptx::named_bar_sync(1, 256);  // the next piece's Q goes where the weights were
+                } else if (last && (two || t == 0)) {
                     auto ml_of = [&](int k) {
-                        return k == me ? make_float2(m, l) : __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr);
+                        return k == me || !live ? make_float2(m, l) : __ldcg(reinterpret_cast<const float2*>(slot_of(k) + kBlock * D) + sr);
                     };
                     // the first kHeld pieces' weights stay in registers
                     constexpr int kHeld = 6;
@@ -923,7 +995,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         for (int z = 1; z < kHeld; ++z) w = k == z ? held[z] : w;
                         return w;
                     };
-                    if (live) finish(M, L);
+                    if (live) finish(M, L, R);
                     // kDims dims of a piece at a time, and after a step's pieces those of
                     // the base, through Q's space: every thread copies and reads its own
                     // row, `depth` ahead (where a step is one copy, no more than the base has
@@ -936,8 +1008,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     auto ask = [&](int slot_no) {
                         if (ask_d < D) {
                             const float4* from = reinterpret_cast<const float4*>(slot_of(ask_k)) + (ask_d / 4) * kBlock + sr;
+                            if (live)
 #pragma unroll
-                            for (int e = 0; e < kDims / 4; ++e) ptx::async_copy16(to + slot_no * kStage + e * (kTile * 16), from + e * kBlock);
+                                for (int e = 0; e < kDims / 4; ++e) ptx::async_copy16(to + slot_no * kStage + e * (kTile * 16), from + e * kBlock);
                             ask_k += ask_k + 1 == me ? 2 : 1;
                             if (ask_k >= n) {
                                 if (a.base_out && live)
