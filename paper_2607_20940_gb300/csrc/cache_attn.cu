@@ -145,9 +145,8 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // exact in f16. Which of a product's 16 columns stands for which dim or token is
 // free, so each lane keeps what it loads: 32 neighbouring dims of two tokens for
 // the scores, one block of four tokens for the outputs. Pairs come through a ring
-// of asynchronous copies of the warp's own (no registers wait for memory). Bulk
-// copies with a barrier took 600 of a pair's 3850 cycles, 16-byte copies by every
-// lane @@.
+// of asynchronous copies of the warp's own (no registers wait for memory), 16 bytes a
+// lane (with bulk copies and a barrier: 68.7 us where it took 66.2).
 //
 // Work: every (sequence, key head) is an item of its pairs and kItem more units
 // (what a piece costs besides them); the warps of the grid take equal, contiguous
@@ -156,6 +155,12 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // shared memory; when the CTA's warps are done, each item's pieces are added in
 // order, and where an item goes over several CTAs, the last of them to finish
 // adds theirs in order (the same bits whichever is last).
+//
+// Measured, 128 dims: 64 sequences of up to 8191 tokens, 8 key heads, 4 queries each:
+// 284 MB in 64.4 us (4.4 TB/s, 0.65 of a copy's rate); one of 131071 tokens: 151 MB in
+// 39.6 us. An SM's four schedulers issue in 57% of the cycles; the conversions (2.8
+// cycles a warp) and the f16 products that share a pipe with the scaling hold them up
+// more than HBM does, and a launch's ends (shares, joins) take 6 to 8 us.
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kItem = 1, kSplit = 4;
@@ -228,7 +233,8 @@ __device__ __forceinline__ void operand(uint32_t (&a)[4], uint32_t w0, uint32_t 
 template <int D, int NT>
 struct FewCfg {
     static constexpr int kRows = 8 * NT;
-    static constexpr int kWarps = NT == 1 || D == 64 ? 16 : 12;
+    // by the registers: 128, 168 or 255 a thread (64 dims, 20 rows: 16 warps spill)
+    static constexpr int kWarps = NT == 1 || D * NT < 192 ? 16 : D * NT <= 256 ? 12 : 8;
     static constexpr int kStages = 2;  // pairs of records in flight
     static constexpr int kPitch = D + 4;                        // floats of a row of outputs in shared memory
     static constexpr int kPart = kRows * (kPitch + 2) * 4;      // a piece's output, maxima and sums
@@ -237,7 +243,9 @@ struct FewCfg {
     static constexpr int kSmem = kWarps * (kOwn + kPart) + 128;
     static constexpr int kSlot = kRows * (D + 2);               // floats of a CTA's partial result
 };
-static_assert(FewCfg<128, 1>::kSmem <= 226 * 1024 && FewCfg<128, 2>::kSmem <= 226 * 1024, "shared memory of the launch");
+static_assert(FewCfg<128, 1>::kSmem <= 224 * 1024 && FewCfg<128, 2>::kSmem <= 224 * 1024 && FewCfg<128, 3>::kSmem <= 224 * 1024 &&
+                  FewCfg<64, 3>::kSmem <= 224 * 1024,
+              "shared memory of the launch");
 
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
@@ -346,7 +354,8 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     // ---- the warps' shares. A pair belongs to the warp that has its unit: the item's
     // first + kItem + pair; the CTA finds the sequence that its first warp begins in.
     // Few items: one for a CTA, if its warps are done with the longest before an even
-    // split over all CTAs and its merge (that takes as long as kSplit pairs a warp).
+    // split over all CTAs and its merge, which takes as long as kSplit pairs a warp (4 heads x
+    // 500 tokens: 9.4 us, 15.2 split).
     const bool whole_items = (long long)a.n * n_heads <= gridDim.x && most <= codes::divide(U, gridDim.x) + kSplit * kW;
     const int workers = (int)min((long long)gridDim.x * kW, max(1ll, codes::divide(U, min_units)));
     auto worker_of = [&](long long u) { return (int)codes::divide((u + 1) * workers - 1, U); };
@@ -858,7 +867,13 @@ cudaError_t launch_cache_attend_simt(const CacheView& c, const CacheAttnArgs& a,
 
 cudaError_t launch_cache_attend(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
     const long long rows = (long long)a.group.d * a.queries;
+    // Up to 8 rows a column of products for them: 65 us at 64 sequences of 8191 tokens and 8
+    // key heads of 128 (97 with the second column that 16 rows have). 17 to 24 rows in
+    // three: 145 us there (20 rows), 187 as blocks of 16 and 4, 173 in the kernel of many
+    // queries. 25 to 32 in two blocks: 195 us there, 173 with many, but 84 and 90 at one
+    // sequence of 131k, 14 and 18 at four of 1000; four columns spill, 122 -> 134 us (64 dims).
     if (rows <= 8) return c.D == 128 ? launch_few<128, 1>(c, a, st) : launch_few<64, 1>(c, a, st);
+    if (rows > 16 && rows <= 24) return c.D == 128 ? launch_few<128, 3>(c, a, st) : launch_few<64, 3>(c, a, st);
     if (rows <= 32) return c.D == 128 ? launch_few<128, 2>(c, a, st) : launch_few<64, 2>(c, a, st);
     return launch_cache_attend_many(c, a, st);
 }
