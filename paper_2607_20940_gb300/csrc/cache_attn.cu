@@ -313,28 +313,33 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             if (w < warp) before += s_scan[w];
             all += s_scan[w];
         }
-        __syncthreads();
         return before + v - x;
     };
 
     // ---- all units, and those before each sequence of the first kT
     long long U = 0, mine = 0;
-    bool none = false;
-    int most = 0;  // units of the longest item
+    int most = 0, least = 1;  // units of the longest item; whether none is empty
     for (int i = threadIdx.x; i < a.n; i += kT) {
         const int x = units_of(length(i));
-        none |= x == 0;
         mine += x;
         most = max(most, x);
+        least = min(least, x);
     }
     most = __reduce_max_sync(0xffffffffu, most);
-    if (lane == 0) s_most[warp] = most;
+    least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) s_most[warp] = least ? most : ~most;
     const long long before_mine = scan(mine, U) * n_heads;
     U *= n_heads;
-    for (int w = 0; w < kW; ++w) most = max(most, s_most[w]);
+    bool none = false;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+        const int x = s_most[w];
+        none |= x < 0;
+        most = max(most, x < 0 ? ~x : x);
+    }
 
     // ---- sequences without tokens: their rows are empty, or the base's
-    if (__syncthreads_or(none))
+    if (none)
         for (long long x = blockIdx.x; x < (long long)a.n * n_heads; x += gridDim.x) {
             const int i = (int)(x / n_heads), hb = (int)(x % n_heads);
             if (length(i) > 0) continue;
@@ -385,6 +390,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 const int i = i0 + (int)threadIdx.x;
                 const long long x = i < a.n ? (long long)units_of(length(i)) * n_heads : 0;
                 long long all;
+                __syncthreads();
                 const long long before = base + scan(x, all);
                 if (cta0 >= before && cta0 < before + x) {
                     s_found[0] = i;
@@ -440,25 +446,13 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 if ((!second || both) && inside) ptx::async_copy16(to + 512 * k, (second ? p1 : p0) + 512 * k);
             }
         };
-        int next = r0;  // pair to ask for
-#pragma unroll
-        for (int s = 0; s < kS; ++s) {
-            if (next < r1) {
-                fetch(next, pages_of(next), s);
-                ++next;
-            }
-            ptx::async_commit();
-        }
-        int2 page_next = next < r1 ? pages_of(next) : make_int2(0, 0);
-
         // ---- queries: row g + 8 nt, dims D / 4 t ...
-        uint32_t qf[NT][D / 16][2];
-        float f[NT][2];    // of rows 2 t and 2 t + 1: to base-2 scores
-        int limit[NT][2];  // tokens that they see
+        // (asked for before the first pairs, whose places take a load of their own)
+        uint32_t wq[NT][D / 8];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = 8 * nt + g;
-            uint32_t w[D / 8];
+            uint32_t(&w)[D / 8] = wq[nt];
             if (r < rows) {
                 const uint16_t* q = a.q + place(a.q_st, seq, hb, r) + t * (D / 4);
 #pragma unroll
@@ -470,6 +464,23 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
 #pragma unroll
                 for (int e = 0; e < D / 8; ++e) w[e] = 0u;
             }
+        }
+        int next = r0;  // pair to ask for
+#pragma unroll
+        for (int s = 0; s < kS; ++s) {
+            if (next < r1) {
+                fetch(next, pages_of(next), s);
+                ++next;
+            }
+            ptx::async_commit();
+        }
+        int2 page_next = next < r1 ? pages_of(next) : make_int2(0, 0);
+        uint32_t qf[NT][D / 16][2];
+        float f[NT][2];    // of rows 2 t and 2 t + 1: to base-2 scores
+        int limit[NT][2];  // tokens that they see
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const uint32_t(&w)[D / 8] = wq[nt];
             uint32_t top = 0;
 #pragma unroll
             for (int e = 0; e < D / 8; ++e) top = max(top, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
@@ -733,11 +744,13 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     };
     // The pieces of an item (a group): warp w0's last, or the CTA's first, and then the
     // first pieces of the warps after it up to `end`. Whether the item goes on in the next CTA.
+    const unsigned through = __ballot_sync(0xffffffffu, lane < kW && s_first[lane < kW ? lane : 0] == 2);
     auto extent = [&](int w0, int last, int& end) {
         end = w0;
-        bool goes_on = last ? true : s_first[w0] == 2;
-        while (goes_on && end + 1 < kW) goes_on = s_first[++end] == 2;
-        return goes_on;
+        if (!last && !(through >> w0 & 1)) return false;
+        const unsigned stops = ~through & ((1u << kW) - 1) & ~((2u << w0) - 1);  // warps after w0 that end an item or have no part in it
+        end = stops ? __ffs(stops) - 1 : kW - 1;
+        return !stops;
     };
     auto slot_at = [&](int k) { return c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot; };
     // A warp weighs a group's pieces, a lane a row: into s_w, and what the whole group
@@ -794,6 +807,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
                 __stcg(reinterpret_cast<float4*>(slot_at(last) + r * D + d), y);
         }
     }
+    if (whole_items) return;
     __syncthreads();
     // Items of several CTAs: this one's pieces are in place.
     if (lane == 0 && warp < 2 && (warp ? over >= 0 : s_first[0] != 0)) {
