@@ -249,7 +249,7 @@ static_assert(FewCfg<128, 1>::kSmem <= 224 * 1024 && FewCfg<128, 2>::kSmem <= 22
 
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
-    cache_few_kernel(const CacheView c, const CacheAttnArgs a, int min_units) {
+    cache_few_kernel(const CacheView c, const CacheAttnArgs a) {
     using C = FewCfg<D, NT>;
     constexpr int kW = C::kWarps, kT = 32 * kW, kS = C::kStages, kRec = cache_record_bytes(D);
     extern __shared__ __align__(128) unsigned char smem[];
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
     // split over all CTAs and its merge, which takes as long as kSplit pairs a warp (4 heads x
     // 500 tokens: 9.4 us, 15.2 split).
     const bool whole_items = (long long)a.n * n_heads <= gridDim.x && most <= codes::divide(U, gridDim.x) + kSplit * kW;
-    const int workers = (int)min((long long)gridDim.x * kW, max(1ll, codes::divide(U, min_units)));
+    const int workers = (int)min((long long)gridDim.x * kW, max(1ll, U));
     auto worker_of = [&](long long u) { return (int)codes::divide((u + 1) * workers - 1, U); };
     int seq;
     long long seq0, u0, u1;  // first unit of the sequence; the warp's units
@@ -379,6 +379,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         auto share = [&](int w) { return w >= workers ? U : codes::divide(U * w, workers); };
         const int me = (int)blockIdx.x * kW + warp;
         const long long cta0 = share((int)blockIdx.x * kW);
+        u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
         if (a.n <= kT) {
             if (cta0 >= before_mine && cta0 < before_mine + mine * n_heads) {
                 s_found[0] = threadIdx.x;
@@ -401,7 +402,6 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             }
         }
         __syncthreads();
-        u0 = me < workers ? share(me) : 0, u1 = me < workers ? share(me + 1) : 0;
         seq = (int)s_found[0];
         seq0 = s_found[1];
     }
@@ -753,30 +753,40 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         return !stops;
     };
     auto slot_at = [&](int k) { return c.partials + (size_t)(2 * blockIdx.x + k) * C::kSlot; };
-    // A warp weighs a group's pieces, a lane a row: into s_w, and what the whole group
-    // has into the item's join, or (items of several CTAs) into the CTA's slot.
+    // A warp weighs a group's pieces, kLanes lanes a row: into s_w, and what the whole
+    // group has into the item's join, or (items of several CTAs) into the CTA's slot.
+    constexpr int kLanes = NT == 1 ? 4 : NT == 2 ? 2 : 1;
     auto weigh = [&](int w0, int last) {
         int end;
         const bool alone = !extent(w0, last, end) && last;
         const int i = alone ? s_alone[w0][0] : s_item[last][0], hb = alone ? s_alone[w0][1] : s_item[last][1];
-        if (lane < rows_of(hb)) {
-            auto ml_of = [&](int w) {
-                return *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * lane);
-            };
-            float M = kLowest, L = 0.f;
-#pragma unroll 4
-            for (int w = w0; w <= end; ++w) M = fmaxf(M, ml_of(w).x);
-#pragma unroll 4
-            for (int w = w0; w <= end; ++w) {
-                const float2 x = ml_of(w);
-                const float k = codes::ex2(x.x - M);
-                s_w[last && w == w0][w][lane] = k;
-                L += k * x.y;
-            }
+        const int r = lane / kLanes, part = lane % kLanes;
+        const bool live = r < rows_of(hb);
+        float2 x[(kW + kLanes - 1) / kLanes];
+        float M = kLowest, L = 0.f;
+#pragma unroll
+        for (int j = 0; j < (kW + kLanes - 1) / kLanes; ++j) {
+            const int w = w0 + part + j * kLanes;
+            x[j] = make_float2(kLowest, 0.f);
+            if (live && w <= end) x[j] = *reinterpret_cast<const float2*>(part_of(w, last && w == w0) + C::kRows * C::kPitch + 2 * r);
+            M = fmaxf(M, x[j].x);
+        }
+#pragma unroll
+        for (int d = 1; d < kLanes; d *= 2) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+#pragma unroll
+        for (int j = 0; j < (kW + kLanes - 1) / kLanes; ++j) {
+            const int w = w0 + part + j * kLanes;
+            const float k = codes::ex2(x[j].x - M);
+            if (live && w <= end) s_w[last && w == w0][w][r] = k;
+            L += k * x[j].y;
+        }
+#pragma unroll
+        for (int d = 1; d < kLanes; d *= 2) L += __shfl_xor_sync(0xffffffffu, L, d);
+        if (live && part == 0) {
             if (alone)
-                finish(w0, i, hb, lane, M, L);
+                finish(w0, i, hb, r, M, L);
             else
-                __stcg(reinterpret_cast<float2*>(slot_at(last) + C::kRows * D + 2 * lane), make_float2(M, L));
+                __stcg(reinterpret_cast<float2*>(slot_at(last) + C::kRows * D + 2 * r), make_float2(M, L));
         }
     };
     if (s_last[warp]) weigh(warp, 1);
@@ -795,7 +805,7 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
         for (int x = threadIdx.x; x < rows_of(hb) * (D / 4); x += kT) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
             for (int w = from; w <= end; ++w) {
                 const float4 z = *reinterpret_cast<const float4*>(part_of(w, last && w == from) + r * C::kPitch + d);
                 const float k = s_w[last && w == from][w][r];
@@ -868,7 +878,7 @@ cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t 
     if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(cache_few_kernel<D, NT>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
-                      st, c, a, 2);
+                      st, c, a);
 }
 
 }  // namespace
