@@ -157,10 +157,11 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // adds theirs in order (the same bits whichever is last).
 //
 // Measured, 128 dims: 64 sequences of up to 8191 tokens, 8 key heads, 4 queries each:
-// 284 MB in 64.4 us (4.4 TB/s, 0.65 of a copy's rate); one of 131071 tokens: 151 MB in
-// 39.6 us. An SM's four schedulers issue in 57% of the cycles; the conversions (2.8
+// 284 MB in 62.9 us (4.5 TB/s, 0.66 of a copy's rate); one of 131071 tokens: 151 MB in
+// 37.2 us. An SM's four schedulers issue in 57% of the cycles; the conversions (2.8
 // cycles a warp) and the f16 products that share a pipe with the scaling hold them up
-// more than HBM does, and a launch's ends (shares, joins) take 6 to 8 us.
+// more than HBM does, and a launch's ends (shares, joins) take 5 to 7 us: a list of two
+// short sequences 5.5 us.
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kItem = 1, kSplit = 4;

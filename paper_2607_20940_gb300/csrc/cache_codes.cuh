@@ -1,5 +1,5 @@
-// Conversions of the 4-bit cache's codes and scales, and the walk of its
-// attention kernels over their share of the work.
+// What the 4-bit cache's attention kernels have in common: conversions of codes
+// and scales, rows of queries in f16, divisions of shares, the join.
 #pragma once
 
 #include <stdint.h>
