@@ -7,6 +7,10 @@
 // by their tiles, form one sequence that the CTAs (one per SM) share evenly. A
 // piece that is not a whole item leaves its unnormalised output, maximum and sum
 // in a slot; the last CTA of an item to finish adds its pieces in order.
+// With more than 256 rows a head and 128 dims, two CTAs (kPair) take blocks of 512 rows
+// together: each has half of the rows, and of every step converts half of the tokens' keys and
+// half of the values' dims; the first one's issuer issues products of 256 rows
+// (cta_group::2), which read half as much of K and V from each shared memory.
 //
 // Roles (512 threads):
 //   warp 0      MMA issuer: S_t = Q_t K^T (both from shared memory), O_t += P_t V
@@ -30,13 +34,14 @@
 // warp that sees it may rescale O_t in place.
 //
 // Bound: the tensor pipe (4 D operations per row and token) with many rows, HBM
-// (9/8 D bytes a token) with few; what holds it up is shared memory, through which Q and
-// K go for every scores, V for every product, and every step's tiles on their way from
-// the codes: 2667 cycles a step of two tiles, whose products take 1024. Measured, 128
-// dims: 12 heads of 3120 queries over 24960 tokens 381 us (1.25 PFLOP/s, 0.66 of the
-// library's rate); causal, 500 to 5099 tokens of three sequences, 4 key heads, 1000
-// queries of 16 heads 52 us (0.75 PFLOP/s), of which a launch's fixed parts are 25.
-// Every wait is bounded.
+// (9/8 D bytes a token) with few. What holds it up, of one CTA: shared memory, through
+// which Q and K go for every scores, V for every product, and every step's tiles on
+// their way from the codes (2667 cycles a step of two tiles, whose products take 1024); of
+// a pair, the chain of softmax (1300), products and barriers of each tile (2300). Measured,
+// 128 dims: 12 heads of 3120 queries over 24960 tokens 342 us (1.40 PFLOP/s, 0.74 of the
+// library's rate); causal, three sequences of 0 to 5099 tokens, 4 key heads, 1000 queries
+// of 16 heads 51 us (0.75 PFLOP/s), of which a launch's fixed parts are 25. Every wait is
+// bounded.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -60,33 +65,40 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr int kLaunchRegs = 128, kCtrlRegs = 80, kCodeRegs = 64, kSoftmaxRegs = 184;
 static_assert(4 * kCtrlRegs + 4 * kCodeRegs + 8 * kSoftmaxRegs <= 16 * kLaunchRegs, "register split");
 
-template <int D>
+// kPair: two CTAs (a cluster) take a block together, each half its rows and half of every
+// tile of K (tokens) and V (dims).
+template <int D, bool kPair>
 struct ManyCfg {
-    static constexpr int kBytes = kTile * D * 2;  // of a tile in shared memory
+    static constexpr int kBytes = kTile * D * 2;  // of a tile of Q in shared memory
+    static constexpr int kRowsK = kPair ? kTile / 2 : kTile, kColsV = kPair ? D / 2 : D;
+    static constexpr int kKV = kTile * kColsV * 2;      // of a tile of K or V
     static constexpr int kCode = 8 * cache_v_codes(D);  // of a step's codes and scales of K, or of V
-    static constexpr int kCodes = D == 128 ? 3 : kMaxCodes;  // half steps that fit beside two tiles of Q
-    static constexpr int kUsed = (2 + kK + kV) * kBytes + kCodes * kCode + 1024;
+    static constexpr int kCodes = kPair ? kMaxCodes : D == 128 ? 3 : kMaxCodes;  // half steps that fit beside two tiles of Q
+    static constexpr int kUsed = 2 * kBytes + (kK + kV) * kKV + kCodes * kCode + 1024;
     static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;  // one CTA per SM (all of TMEM)
     // with one tile of Q its second is room for more
     static constexpr int kCodes1 = kCodes + kBytes / kCode < kMaxCodes ? kCodes + kBytes / kCode : kMaxCodes;
     static constexpr size_t kSlot = (size_t)kBlock * (D + 2);  // floats of a partial result
 };
-static_assert(ManyCfg<128>::kSmem + 1024 <= 227 * 1024, "shared memory of the launch");
-static_assert(2 * 160 * ManyCfg<128>::kSlot <= kCachePartialFloats, "partial results");
+static_assert(ManyCfg<128, false>::kSmem + 1024 <= 227 * 1024 && ManyCfg<128, true>::kSmem + 1024 <= 227 * 1024, "shared memory of the launch");
+static_assert(2 * 160 * ManyCfg<128, false>::kSlot <= kCachePartialFloats, "partial results");
 
 // A CTA's pieces of the call's items, in order. One warp finds them and hands them
 // to the others through a ring in shared memory.
 struct Piece {
     int seq, hk, blk;   // row of the list, key head, block
     int len;            // of the sequence
-    int rows, tiles;    // of the block
+    int row0, rows;     // of this CTA's part of the block: the first, of the key head's rows, and how many
+    int tiles;          // of it (of a pair's longer part)
     int steps, b0, b1;  // of the item; this piece's. steps 0: no more
     int item0;          // the item's first unit, from the CTA's first
 };
 constexpr int kPieces = 4;
-// What an item costs besides its steps, in steps of a tile (3: prompts 62 us, 6: 51, 9: 50, but
-// 32 sequences of 60 rows 57, 58 and 59).
-constexpr int kItem = 6;
+// What an item costs besides its steps, in steps of a tile (one CTA's, 3: prompts 62 us, 6: 51,
+// 9: 50, but 32 sequences of 60 rows 57, 58 and 59; a pair's, 6: 53, 9: 51, 32 sequences of
+// 512 rows 51 and 47).
+template <bool kPair>
+constexpr int kItemOf = kPair ? 9 : 6;
 // Pieces of an item of one tile up to which a thread adds a row's (100 rows x 100k tokens 143 us so,
 // 92 by both warpgroups; two tiles' threads are busy as it is: 400 rows x 2000 tokens 34 and 45 us).
 constexpr int kRowMerge = 4;
@@ -94,7 +106,10 @@ constexpr int kRowMerge = 4;
 // 16: 23; 20: 100 rows x 3000 tokens 37 us, 16: 31).
 constexpr int kSplit = 16;
 
+template <bool kPair>
 struct Shape {
+    static constexpr int kRows = kPair ? 2 * kBlock : kBlock;  // of a block
+    static constexpr int kItem = kItemOf<kPair>;
     const CacheView& c;
     const CacheAttnArgs& a;
     const FastDiv& by_block;  // blocks of a (sequence, key head)
@@ -106,10 +121,12 @@ struct Shape {
         const int s = a.seqs ? a.seqs[i] : i;
         return (unsigned)s < (unsigned)c.S ? max(0, min(c.lengths[s], c.W * c.P) - a.skip) : 0;
     }
-    __device__ int block_rows(int b) const { return min(kBlock, rows - b * kBlock); }
-    __device__ int tiles(int b) const { return (block_rows(b) + kTile - 1) / kTile; }
+    __device__ int block_rows(int b) const { return min(kRows, rows - b * kRows); }
+    // of the block's rows, the first CTA's
+    __device__ int part(int b) const { return kPair ? min(block_rows(b), (block_rows(b) + 15) / 16 * 8) : block_rows(b); }
+    __device__ int tiles(int b) const { return (part(b) + kTile - 1) / kTile; }
     __device__ int steps(int n, int b) const {
-        if (a.causal) n = min(n, max(0, n - a.queries + 1 + a.group.div(b * kBlock + block_rows(b) - 1)));
+        if (a.causal) n = min(n, max(0, n - a.queries + 1 + a.group.div(b * kRows + block_rows(b) - 1)));
         return (n + kTile - 1) / kTile;
     }
     // Units of an item: a step of one tile, and kItem for what it costs besides its steps.
@@ -119,16 +136,20 @@ struct Shape {
     }
 };
 
-template <int D>
+template <int D, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView c, const CacheAttnArgs a, const FastDiv by_block,
                                                                  long long wait_limit) {
-    using C = ManyCfg<D>;
+    using C = ManyCfg<D, kPair>;
+    constexpr int kItem = kItemOf<kPair>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* sK = smem;
-    unsigned char* sV = sK + kK * C::kBytes;
-    unsigned char* sQ = sV + kV * C::kBytes;
-    const bool one_tile = a.group.d * a.queries <= kTile;
+    unsigned char* sV = sK + kK * C::kKV;
+    unsigned char* sQ = sV + kV * C::kKV;
+    const bool one_tile = !kPair && a.group.d * a.queries <= kTile;
+    const int rank = kPair ? (int)ptx::cluster_rank() : 0;  // in the pair
+    // the CTAs, or pairs, that share the work
+    const int n_workers = (int)gridDim.x / (kPair ? 2 : 1), worker = (int)blockIdx.x / (kPair ? 2 : 1);
     unsigned char* sC = sQ + (one_tile ? 1 : 2) * C::kBytes;
     const int n_codes = one_tile ? C::kCodes1 : C::kCodes;
     __shared__ uint64_t c_full[kMaxCodes], c_empty[kMaxCodes], q_full, k_full[kK], k_empty[kK], v_full[kV], v_empty[kV];
@@ -146,13 +167,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        ptx::mbar_init(&q_full, 8);
+        constexpr int kCtas = kPair ? 2 : 1;  // whose warps arrive where the issuer waits
+        ptx::mbar_init(&q_full, 8 * kCtas);
         for (int s = 0; s < kK; ++s) {
-            ptx::mbar_init(&k_full[s], 2);
+            ptx::mbar_init(&k_full[s], 2 * kCtas);
             ptx::mbar_init(&k_empty[s], 1);
         }
         for (int s = 0; s < kV; ++s) {
-            ptx::mbar_init(&v_full[s], 2);
+            ptx::mbar_init(&v_full[s], 2 * kCtas);
             ptx::mbar_init(&v_empty[s], 1);
         }
         for (int s = 0; s < kMaxCodes; ++s) {
@@ -161,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         }
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&s_full[t], 1);
-            ptx::mbar_init(&p_full[t], 4);
+            ptx::mbar_init(&p_full[t], 4 * kCtas);
         }
         for (int s = 0; s < kPieces; ++s) {
             ptx::mbar_init(&pc_full[s], 1);
@@ -172,18 +194,26 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         ptx::fence_mbar_init();
     }
     if (warp == 1) {
-        ptx::tmem_alloc(&tmem_base_sh, 512);
-        ptx::tmem_relinquish();
+        if constexpr (kPair) {
+            ptx::tmem_alloc_pair(&tmem_base_sh, 512);
+            ptx::tmem_relinquish_pair();
+        } else {
+            ptx::tmem_alloc(&tmem_base_sh, 512);
+            ptx::tmem_relinquish();
+        }
     }
     ptx::tc_fence_before();
     __syncthreads();
+    if constexpr (kPair) ptx::cluster_sync();  // the other's barriers are in place
     ptx::tc_fence_after();
     const uint32_t tbase = tmem_base_sh;
     volatile int* abort_p = &abort_flag;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
-    const Shape shape(c, a, by_block);
+    const Shape<kPair> shape(c, a, by_block);
+    // Arrive where the issuer waits.
+    auto arrive = [](uint64_t* bar) { kPair ? ptx::mbar_arrive_first(bar) : ptx::mbar_arrive(bar); };
     auto place = [&](const long long* st, int i, int hk, int r) {
         const int t = a.group.div(r);
         return i * st[0] + t * st[1] + (hk * a.group.d + r - t * a.group.d) * st[2];
@@ -240,15 +270,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         most = max(most, x < 0 ? ~x : x);
     }
     const long long U = U1 * c.Hk;
-    const int G = (int)min((long long)gridDim.x, max(1ll, U / 2));  // a share of two units holds a step of any item
-    bool idle = (int)blockIdx.x >= G || U == 0;
-    long long u0 = idle ? 0 : codes::divide(U * blockIdx.x, G), u1 = idle ? 0 : codes::divide(U * (blockIdx.x + 1), G);
+    const int G = (int)min((long long)n_workers, max(1ll, U / 2));  // a share of two units holds a step of any item
+    bool idle = worker >= G || U == 0;
+    long long u0 = idle ? 0 : codes::divide(U * worker, G), u1 = idle ? 0 : codes::divide(U * (worker + 1), G);
     // Few items: one for a CTA, if the longest is done before an even split and its merge.
-    const bool whole_items = items <= gridDim.x && most - kItem <= codes::divide(U, gridDim.x) + kSplit;
+    const bool whole_items = items <= n_workers && most - kItem <= codes::divide(U, n_workers) + kSplit;
     if (whole_items) {
-        idle = (int)blockIdx.x >= items;
+        idle = worker >= items;
         if (threadIdx.x == 0 && !idle) {
-            const int hk = (int)blockIdx.x / (int)items1, x = (int)blockIdx.x - hk * (int)items1, i = by_block.div(x);
+            const int hk = worker / (int)items1, x = worker - hk * (int)items1, i = by_block.div(x);
             s_begin[0] = hk, s_begin[1] = i, s_begin[2] = x - i * shape.blocks, s_begin[3] = 0;
             s_units[0] = 0, s_units[1] = units_of(x);
         }
@@ -319,7 +349,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         const int b1 = end > from ? min(steps, (end - from + w - 1) / w) : 0;
                         if (b0 < b1) {
                             p.seq = seq, p.hk = hk, p.blk = blk, p.len = len;
-                            p.rows = shape.block_rows(blk), p.tiles = w, p.steps = steps;
+                            p.row0 = blk * shape.kRows + rank * shape.part(blk);
+                            p.rows = rank ? shape.block_rows(blk) - shape.part(blk) : shape.part(blk);
+                            p.tiles = w, p.steps = steps;
                             p.b0 = b0, p.b1 = b1, p.item0 = at;
                         }
                         if (steps > 0) at += kItem + steps * w;
@@ -344,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (lane == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
                 const int n = shape.block_rows(b);
                 for (int y = lane; y < n * (D / 8); y += 32) {
-                    const int r = b * kBlock + y / (D / 8), d = y % (D / 8) * 8;
+                    const int r = b * shape.kRows + y / (D / 8), d = y % (D / 8) * 8;
                     uint4 w = make_uint4(0u, 0u, 0u, 0u);
                     if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
                         w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
@@ -352,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
                 if (a.lse && a.lse != a.base_lse)
                     for (int y = lane; y < n; y += 32) {
-                        const long long at = lse_place(i, hk, b * kBlock + y);
+                        const long long at = lse_place(i, hk, b * shape.kRows + y);
                         a.lse[at] = a.base_lse ? a.base_lse[at] : -INFINITY;
                     }
             }
@@ -365,6 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                                       (long long)pc.hk * (c.P / 16) * cache_record_bytes(D);
                 for (int j = pc.b0; j < pc.b1 && ok; ++j) {
                     const int r = 8 * j + lane, n = min(8, (pc.len + 15) / 16 - 8 * j);
+                    const int k0 = kPair ? 4 * rank : 0, k1 = kPair ? min(n, k0 + 4) : n;  // records whose keys are wanted
                     const uint8_t* rec = from;
                     if (lane < n) {
                         const int page = row[r >> (c.log2_p - 4)];
@@ -375,9 +408,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         const int sl = half % n_codes;
                         ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&c_empty[sl], (uint32_t)(half / n_codes & 1) ^ 1u, abort_p, wait_limit));
                         if (!ok) break;
-                        if (lane == 0) ptx::mbar_arrive_expect_tx(&c_full[sl], (uint32_t)(n * cache_v_codes(D)));
+                        const int l0 = v ? 0 : k0, l1 = v ? n : k1;
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(&c_full[sl], (uint32_t)(max(0, l1 - l0) * cache_v_codes(D)));
                         __syncwarp();
-                        if (lane < n)
+                        if (lane >= l0 && lane < l1)
                             ptx::bulk_load(sC + sl * C::kCode + lane * cache_v_codes(D), rec + v * cache_v_codes(D), cache_v_codes(D), &c_full[sl]);
                     }
                 }
@@ -391,11 +425,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ptx::mbar_wait_bounded(&c_full[i % n_codes], (uint32_t)(i / n_codes & 1), &never, kWaitLimit);
                 if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
             }
+        } else if (warp == 0 && rank != 0) {
+            for (int n = 0; piece(n, pc); ++n) done(n);  // the pair's first CTA issues
         } else if (warp == 0) {
             // ============================= MMA issuer =============================
-            constexpr uint32_t idS = ptx::idesc_f16(kTile, kTile, false, false);
-            constexpr uint32_t idO = ptx::idesc_f16(kTile, D, false, true);
-            constexpr uint64_t kTileDesc = (uint64_t)(C::kBytes >> 4);
+            constexpr int kM = kPair ? 2 * kTile : kTile;
+            constexpr uint32_t idS = ptx::idesc_f16(kM, kTile, false, false);
+            constexpr uint32_t idO = ptx::idesc_f16(kM, D, false, true);
+            constexpr uint64_t kTileDesc = (uint64_t)(C::kBytes >> 4), kKVDesc = (uint64_t)(C::kKV >> 4);
             const uint64_t q_desc = ptx::sdesc_sw128(ptx::smem_u32(sQ), 16, 1024);
             const uint64_t k_desc = ptx::sdesc_sw128(ptx::smem_u32(sK), 16, 1024);
             const uint64_t v_desc = ptx::sdesc_sw128(ptx::smem_u32(sV), kTile * 128, 1024);
@@ -403,21 +440,30 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 const bool r = ptx::mbar_wait_bounded(bar, parity, abort_p, wait_limit);
                 return __all_sync(0xffffffffu, r);
             };
+            auto commit = [](uint64_t* bar) { kPair ? ptx::mma_commit_pair(bar) : ptx::mma_commit(bar); };
             auto issue_s = [&](int t, int st, int qt) {  // S_t = Q_qt K^T
-                const uint64_t kd = k_desc + (uint64_t)st * kTileDesc, qd = q_desc + (uint64_t)qt * kTileDesc;
+                const uint64_t kd = k_desc + (uint64_t)st * kKVDesc, qd = q_desc + (uint64_t)qt * kTileDesc;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint64_t off = (uint64_t)(((kk / 4) * (kTile * 128) + (kk % 4) * 32) >> 4);
-                    ptx::mma_ss(tbase + t * 128, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
+                    const uint64_t koff = (uint64_t)(((kk / 4) * (C::kRowsK * 128) + (kk % 4) * 32) >> 4);
+                    if constexpr (kPair)
+                        ptx::mma_ss_pair(tbase + t * 128, qd + off, kd + koff, idS, kk > 0 ? 1u : 0u);
+                    else
+                        ptx::mma_ss(tbase + t * 128, qd + off, kd + koff, idS, kk > 0 ? 1u : 0u);
                 }
-                ptx::mma_commit(&s_full[t]);
+                commit(&s_full[t]);
             };
             auto issue_o = [&](int t, int st, bool more) {  // O_t += P_t V
-                const uint64_t vd = v_desc + (uint64_t)st * kTileDesc;
+                const uint64_t vd = v_desc + (uint64_t)st * kKVDesc;
 #pragma unroll
-                for (int kk = 0; kk < kTile / 16; ++kk)
-                    ptx::mma_ts(tbase + 256 + t * 128, tbase + t * 128 + kk * 8, vd + (uint64_t)(kk * (2048 >> 4)), idO,
-                                (more || kk > 0) ? 1u : 0u);
+                for (int kk = 0; kk < kTile / 16; ++kk) {
+                    const uint32_t d = tbase + 256 + t * 128, p = tbase + t * 128 + kk * 8, add = (more || kk > 0) ? 1u : 0u;
+                    if constexpr (kPair)
+                        ptx::mma_ts_pair(d, p, vd + (uint64_t)(kk * (2048 >> 4)), idO, add);
+                    else
+                        ptx::mma_ts(d, p, vd + (uint64_t)(kk * (2048 >> 4)), idO, add);
+                }
             };
             static_assert(kK == 2 && kV == 2, "slots take turns");
             // Slots and phases of the next K and V tile and of each P.
@@ -432,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (ptx::elect_one_sync()) {
                     issue_s(0, st, 0);
                     if (two) issue_s(1, st, 1);
-                    ptx::mma_commit(&k_empty[st]);
+                    commit(&k_empty[st]);
                 }
                 __syncwarp();
                 if (two) {
@@ -463,8 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         if (ptx::elect_one_sync()) {
                             issue_o(1, st, j > 0);
                             if (more) issue_s(1, st1, 1);
-                            ptx::mma_commit(&v_empty[st]);
-                            if (more) ptx::mma_commit(&k_empty[st1]);
+                            commit(&v_empty[st]);
+                            if (more) commit(&k_empty[st1]);
                         }
                         __syncwarp();
                         st = st1;
@@ -479,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         ptx::tc_fence_after();
                         if (ptx::elect_one_sync()) {
                             issue_s(j & 1, sk, 0);
-                            ptx::mma_commit(&k_empty[sk]);
+                            commit(&k_empty[sk]);
                         }
                         __syncwarp();
                         return true;
@@ -497,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         ptx::tc_fence_after();
                         if (ptx::elect_one_sync()) {
                             issue_o(t, sv, j > 1);
-                            ptx::mma_commit(&v_empty[sv]);
+                            commit(&v_empty[sv]);
                         }
                         __syncwarp();
                         if (j + 2 < n) ok = scores(j + 2);
@@ -506,14 +552,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     st ^= n & 1;
                 }
                 if (!ok) break;
-                if (ptx::elect_one_sync()) ptx::mma_commit(&o_full);
+                if (ptx::elect_one_sync()) commit(&o_full);
                 done(pieces);
                 ++pieces;
             }
             if (!ok) {
                 // every product issued is done before its operands' space goes
                 if (lane == 0) atomicOr(c.head + kCacheStatus, kDevTimeout);
-                if (ptx::elect_one_sync()) ptx::mma_commit(&drained);
+                if (ptx::elect_one_sync()) commit(&drained);
                 __syncwarp();
                 volatile int never = 0;
                 ptx::mbar_wait_bounded(&drained, 0, &never, kWaitLimit);
@@ -527,20 +573,21 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         // has the same token and dims of every kRecStep-th record. Eight lanes take
         // four tokens and two chunks of 32 dims, so that their 16-byte stores lie in
         // eight different slots of the swizzled rows.
-        constexpr int kPer = 16 * (D / 32);   // units of a record
-        constexpr int kRecStep = 64 / kPer;   // records that a pair of warps takes at a time
-        constexpr int kBatch = 4, kBatches = 8 / kRecStep / kBatch;
+        // Of a pair, each has half of the tokens' keys and half of the values' dims.
         const bool values = warp >= 6;
         const int x = (int)threadIdx.x % 64;
-        const int chunk = (x & 1) + (D == 128 ? x >> 2 & 2 : 0);
-        const int rest = (x >> 1 & 3) + (D == 128 ? x >> 4 << 2 : x >> 3 << 2);  // token among kRecStep records'
-        const int tok = rest % 16, rec0 = rest / 16;
-        const uint32_t codes_at = rec0 * cache_v_codes(D) + tok * (D / 2) + (values ? cache_v_code_at(D, tok, chunk * 16) : chunk * 16);
-        const uint32_t scales_at = rec0 * cache_v_codes(D) + cache_k_scales(D) +
-                                   (values ? chunk * 32 + cache_v_scale_at(tok) : tok * (D / 16) + chunk * 2);
+        const bool four = D == 128 && !(kPair && values);  // chunks of 32 dims a token: four, or two
+        const int chunk = (x & 1) + (four ? x >> 2 & 2 : 0);
+        const int rest = (x >> 1 & 3) + (four ? x >> 4 << 2 : x >> 3 << 2);  // token among the records taken at a time
+        const int tok = rest % 16, rec0 = rest / 16, rec_step = four ? 1 : 2;
+        const int from_chunk = chunk + (kPair && values ? 2 * rank : 0), from_rec = rec0 + (kPair && !values ? 4 * rank : 0);
+        constexpr int kBatch = 4, kBatches = kPair || D == 64 ? 1 : 2;
+        const uint32_t codes_at = from_rec * cache_v_codes(D) + tok * (D / 2) + (values ? cache_v_code_at(D, tok, from_chunk * 16) : from_chunk * 16);
+        const uint32_t scales_at = from_rec * cache_v_codes(D) + cache_k_scales(D) +
+                                   (values ? from_chunk * 32 + cache_v_scale_at(tok) : tok * (D / 16) + from_chunk * 2);
         const uint32_t second = values ? 16 : 1;  // from a unit's first scale to its second
-        const int row0 = 16 * rec0 + tok;  // of the tile; the next is 16 kRecStep rows on
-        const uint32_t tile_at = (uint32_t)((chunk >> 1) * (kTile * 128) + row0 * 128);
+        const int row0 = 16 * rec0 + tok;  // of the tile; the next is 16 rec_step rows on
+        const uint32_t tile_at = (uint32_t)((chunk >> 1) * ((values ? kTile : C::kRowsK) * 128) + row0 * 128);
         const uint32_t slot = (uint32_t)(((chunk & 1) * 4) ^ (row0 & 7)) << 4;
         int n_tiles = 0, pieces = 0;
         // Half of step n_tiles: its codes in the ring to f16 in `tile`. left: tokens
@@ -557,10 +604,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 uint32_t sc[kBatch];
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    const unsigned char* rec = src + (b * kBatch + i) * (kRecStep * cache_v_codes(D));
+                    const unsigned char* rec = src + (b * kBatch + i) * (rec_step * cache_v_codes(D));
                     w[i] = *reinterpret_cast<const uint4*>(rec + codes_at);
                     sc[i] = rec[scales_at] | (uint32_t)rec[scales_at + second] << 8;
-                    if (values && row0 + 16 * kRecStep * (b * kBatch + i) >= left) sc[i] = 0;
+                    if (values && row0 + 16 * rec_step * (b * kBatch + i) >= left) sc[i] = 0;
                 }
                 if (b == kBatches - 1) {
                     __syncwarp();
@@ -579,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                         o.y = codes::mul_f16x2(codes::e2m1_f16x2<1>(cw[q]), sq);
                         o.z = codes::mul_f16x2(codes::e2m1_f16x2<2>(cw[q]), sq);
                         o.w = codes::mul_f16x2(codes::e2m1_f16x2<3>(cw[q]), sq);
-                        *reinterpret_cast<uint4*>(to + (slot ^ (uint32_t)(q << 4)) + (b * kBatch + i) * (16 * kRecStep * 128)) = o;
+                        *reinterpret_cast<uint4*>(to + (slot ^ (uint32_t)(q << 4)) + (b * kBatch + i) * (16 * rec_step * 128)) = o;
                     }
                 }
             }
@@ -591,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         auto give = [&](uint64_t* bar) {
             ptx::fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar);
+            if (lane == 0) arrive(bar);
         };
         static_assert(kK == kV, "one count of tiles");
         unsigned char* const tiles = values ? sV : sK;
@@ -600,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             for (int j = pc.b0; j < pc.b1; ++j, ++n_tiles) {
                 const int st = n_tiles % kK;
                 if (!room(&bar_empty[st], (uint32_t)(n_tiles / kK & 1))) break;
-                convert(tiles + st * C::kBytes, pc.len - j * kTile);
+                convert(tiles + st * C::kKV, pc.len - j * kTile);
                 if (!ok) break;
                 give(&bar_full[st]);
             }
@@ -618,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         int ns = 0, pieces = 0;
         while (piece(pieces, pc)) {
             bool two = pc.tiles == 2;
-            int br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br;  // row of the block, of (sequence, key head)
+            int br = (two ? t * kTile : 0) + r, R = pc.row0 + br;  // row of the CTA's part, of (sequence, key head)
             bool live = br < pc.rows;
             const int limit = !live ? 0x7fffffff : a.causal ? pc.len - a.queries + 1 + a.group.div(R) : pc.len;  // tokens that the row sees
             float f;  // to base-2 scores
@@ -668,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 ptx::fence_proxy_async_smem();
             }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&q_full);
+            if (lane == 0) arrive(&q_full);
 
             float m = kLowest, l = 0.f;
             {
@@ -754,15 +801,17 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ptx::tmem_wait_st();
                     ptx::tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(&p_full[t]);
+                    if (lane == 0) arrive(&p_full[t]);
                 }
             }
             if (!two && t == 1 && pc.b1 - pc.b0 > 1) s_odd[r] = make_float2(m, l);
+            // (A pair's CTAs do so each for its rows.)
+            auto counter_of = [&](int first) { return c.counters + (kPair ? 2 * first + rank : first); };
             // An item of several CTAs: its first, and how many. The last of them to come here
             // adds the others' results, which they leave in slots, to its own.
             auto ctas_of = [&](const Piece& p, int& n) {
                 const long long all = s_units[0], u = s_units[1] + p.item0 + kItem;
-                const int ctas = (int)min((long long)gridDim.x, max(1ll, all / 2));
+                const int ctas = (int)min((long long)n_workers, max(1ll, all / 2));
                 auto cta_of = [&](long long v) { return (int)codes::divide((v + 1) * ctas - 1, all); };
                 const int first = cta_of(u);
                 n = cta_of(u + (long long)(p.steps - 1) * p.tiles) - first + 1;
@@ -773,7 +822,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (p.b0 > 0 || p.b1 < p.steps) {
                     int n;
                     const int first = ctas_of(p, n);
-                    s_last[pieces & 1] = (atomicAdd(c.counters + first, 1u) & 0xffffu) == (unsigned)n - 1;
+                    s_last[pieces & 1] = (atomicAdd(counter_of(first), 1u) & 0xffffu) == (unsigned)n - 1;
                 }
             }
             ok = ok && ptx::mbar_wait_bounded(&o_full, (uint32_t)(pieces & 1), abort_p, wait_limit);
@@ -781,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             if (!ok) break;
             // read again instead of being held over the steps, which have no register to spare
             pc = ring[pieces % kPieces];
-            two = pc.tiles == 2, br = (two ? t * kTile : 0) + r, R = pc.blk * kBlock + br, live = br < pc.rows;
+            two = pc.tiles == 2, br = (two ? t * kTile : 0) + r, R = pc.row0 + br, live = br < pc.rows;
             ptx::tc_fence_after();
 
             // ---- the piece's result
@@ -883,19 +932,19 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 if (!whole && live) __stcg(reinterpret_cast<float2*>(slot + kBlock * D) + sr, make_float2(m, l));
             }
             if (!whole) {
-                const int me = (int)blockIdx.x - first;
+                const int me = worker - first;
                 // c.counters: pieces that came, and pieces in their slots times 2^16
                 if (!last) {
                     ptx::named_bar_sync(1, 256);
                     if (threadIdx.x == 256) {
                         __threadfence();
-                        atomicAdd(c.counters + first, 1u << 16);
+                        atomicAdd(counter_of(first), 1u << 16);
                     }
                 } else {
                     // the others have come, so they write (or have written) and wait for nothing
                     if (threadIdx.x == 256) {
                         const long long t0 = clock64();
-                        volatile unsigned* count = c.counters + first;
+                        volatile unsigned* count = counter_of(first);
                         while (*count >> 16 != (unsigned)n - 1 && ok) ok = clock64() - t0 < wait_limit;
                         if (ok)
                             *count = 0;  // for the next launch
@@ -906,7 +955,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     ok = ptx::named_bar_and(1, 256, ok);
                     if (!ok) break;
                 }
-                auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
+                auto slot_of = [&](int k) { return c.partials + (size_t)(2 * (kPair ? 2 * (first + k) + rank : first + k) + (k == 0 ? 1 : 0)) * C::kSlot; };
                 if (last && shared) {
                     // Many pieces: all 256 threads share the rows' dims, four of a row at a time,
                     // kDeep copies ahead through Q's space, where the weights of some rows are too.
@@ -933,7 +982,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                                 table[k * rows + x] = w;
                                 L += w * ml.y;
                             }
-                            finish(M, L, pc.blk * kBlock + row);
+                            finish(M, L, pc.row0 + row);
                             s_own[x] = jn.own, s_other[x] = jn.other;
                         }
                         ptx::named_bar_sync(1, 256);
@@ -963,7 +1012,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                                 ask(slot_no);
                                 slot_no = slot_no + 1 == kDeep ? 0 : slot_no + 1;
                             }
-                            const long long at = place(a.o_st, pc.seq, pc.hk, pc.blk * kBlock + row0 + row) + 4 * d;
+                            const long long at = place(a.o_st, pc.seq, pc.hk, pc.row0 + row0 + row) + 4 * d;
                             const float ow = s_own[row], other = s_other[row];
                             acc.x *= ow, acc.y *= ow, acc.z *= ow, acc.w *= ow;
                             if (other != 0.f) {
@@ -1095,26 +1144,39 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __syncwarp();
     ptx::tc_fence_before();
     __syncthreads();
+    if constexpr (kPair) ptx::cluster_sync();  // no product or arrival of the other's comes here any more
     if (warp == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tbase, 512);
+        if constexpr (kPair)
+            ptx::tmem_dealloc_pair(tbase, 512);
+        else
+            ptx::tmem_dealloc(tbase, 512);
     }
 }
 
-template <int D>
+template <int D, bool kPair>
 cudaError_t launch_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
+    using C = ManyCfg<D, kPair>;
     int sms;
     cudaError_t e = device_sms(&sms);
-    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_many_kernel<D>, ManyCfg<D>::kSmem, -1, kLaunchRegs);
+    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_many_kernel<D, kPair>, C::kSmem, -1, kLaunchRegs);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_many_kernel<D>, dim3(sms < 160 ? sms : 160), dim3(kThreads), ManyCfg<D>::kSmem, st, c, a,
-                      FastDiv((int)(((long long)a.group.d * a.queries + kBlock - 1) / kBlock)), kWaitLimit);
+    const int rows = Shape<kPair>::kRows;
+    const FastDiv blocks((int)(((long long)a.group.d * a.queries + rows - 1) / rows));
+    const dim3 grid((sms < 160 ? sms : 160) & (kPair ? ~1 : ~0));
+    return kPair ? launch_pdl_cluster(cache_many_kernel<D, kPair>, grid, dim3(kThreads), C::kSmem, st, dim3(2), c, a, blocks, kWaitLimit)
+                 : launch_pdl(cache_many_kernel<D, kPair>, grid, dim3(kThreads), C::kSmem, st, c, a, blocks, kWaitLimit);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_attend_many(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
-    return c.D == 128 ? launch_many<128>(c, a, st) : launch_many<64>(c, a, st);
+    // Pairs of CTAs for blocks of more rows than one has, over longer sequences (what a
+    // sequence can hold is what the host knows): 12 heads of 3120 rows x 24960 tokens 342 us (379 without), 4 of
+    // 300 x 60000 119 (140), 780 x 1560 32.2 (33.2), but 400 x 1000 23.9 (23.2), 1000 x 1000 25.0 (23.8).
+    const bool pair = c.D == 128 && (long long)a.group.d * a.queries > kBlock && (long long)c.W * c.P >= 1536;
+    if (pair) return launch_many<128, true>(c, a, st);
+    return c.D == 128 ? launch_many<128, false>(c, a, st) : launch_many<64, false>(c, a, st);
 }
 
 }  // namespace msf

@@ -93,3 +93,41 @@ def test_a_wait_that_gave_up_is_reported():
     lens = [40, 0, 3, 100]
     kh, vh = fill(c, lens, 61)
     check(c, kh, vh, lens, rows((4, 2, 2, 64), 62))
+
+
+@pytest.mark.parametrize("group,queries", [(1, 257), (3, 100), (2, 192), (4, 128), (1, 513), (5, 140), (1, 1100)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_blocks_of_two(group, queries, causal):
+    """Over sequences that may hold 1536 tokens or more, more than 256 rows go to pairs of blocks of threads."""
+    lens = [0, 1, 15, 17, 64, 65, 113, 128, 129, 500, 1600]
+    c = make(kv_heads=2, head_dim=128, page_tokens=32, sequences=len(lens), sequence_pages=50, pages=120)
+    kh, vh = fill(c, lens, 71)
+    q = rows((len(lens), queries, 2 * group, 128), 72)
+    check(c, kh, vh, lens, q, causal)
+    seqs = [10, 3, 10, 0]
+    base = rows((4, *q.shape[1:]), 73)
+    base_lse = torch.randn(4, 2 * group, queries, generator=torch.Generator().manual_seed(74)).cuda() * 2 + 4
+    base_lse[1, 0, 0] = base_lse[3, 1, 2] = -math.inf
+    wide = torch.zeros(4, queries + 3, 2 * group, 128 + 8, dtype=torch.bfloat16, device="cuda")
+    strided = wide[:, 1:1 + queries, :, 8:]
+    strided.copy_(q[:4])
+    first = check(c, kh, vh, lens, strided, causal, base, base_lse, scale=0.2, seqs=seqs)
+    for _ in range(2):
+        again = torch.empty_like(base), torch.empty_like(base_lse)
+        c.attend(0, strided, *again, base, base_lse, ints(seqs), causal, 0.2)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
+def test_blocks_of_two_with_scores_far_apart():
+    """Every 40th key is far ahead, so maxima move late and by much."""
+    n, queries = 1700, 300
+    c = make(kv_heads=1, head_dim=128, page_tokens=64, sequences=1, sequence_pages=32, pages=32)
+    k, v = rows((1, n, 1, 128), 81, 0.2), rows((1, n, 1, 128), 82)
+    k[:, ::40] *= torch.linspace(1, 30, len(range(0, n, 40)), device="cuda", dtype=torch.bfloat16)[None, :, None, None]
+    c.grow(None, ints([n]))
+    c.write(0, k, v)
+    ok(c)
+    k0, v0 = torch.empty_like(k), torch.empty_like(v)
+    c.read(0, k0, v0)
+    for causal in (False, True):
+        check(c, f64(k0), f64(v0), [n], rows((1, queries, 1, 128), 83, 3.0), causal, floor=2.0 ** -30)
