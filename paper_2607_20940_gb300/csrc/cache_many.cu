@@ -102,6 +102,10 @@ constexpr int kItemOf = kPair ? 9 : 6;
 // Pieces of an item of one tile up to which a thread adds a row's (100 rows x 100k tokens 143 us so,
 // 92 by both warpgroups; two tiles' threads are busy as it is: 400 rows x 2000 tokens 34 and 45 us).
 constexpr int kRowMerge = 4;
+// Units that a piece's addition takes: of two tiles, and for each row of one. (None: shares as
+// small as they get, 200 rows x 4000 tokens 138 us, so 37; 64 x 4847, 24 items, 32 and 29; half: 40 and
+// 30, twice and more: 37 and 30 to 34.)
+constexpr float kAddTwo = 3.75f, kAddOne = 0.014f;
 // Units that writing and adding partial results takes as long as (12: 400 rows x 1000 tokens 31 us,
 // 16: 23; 20: 100 rows x 3000 tokens 37 us, 16: 31).
 constexpr int kSplit = 16;
@@ -162,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __shared__ long long s_scan[kThreads / 32];
     __shared__ int s_most[kThreads / 32];
     __shared__ long long s_units[2];  // all units; this CTA's first
+    __shared__ int s_shares;
     __shared__ int s_begin[4];  // the item that the share begins in: key head, row of the list, block, its first unit from the share's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -270,7 +275,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
         most = max(most, x < 0 ? ~x : x);
     }
     const long long U = U1 * c.Hk;
-    const int G = (int)min((long long)n_workers, max(1ll, U / 2));  // a share of two units holds a step of any item
+    // An item of k units by shares of m takes m, and k / m pieces' addition, each as long as
+    // `add` units: least at m = sqrt(k add). (A share of two units holds a step of any item.)
+    const int tile_rows = min(shape.rows, kTile);
+    const float add = shape.tiles(0) == 2 ? kAddTwo : kAddOne * tile_rows;
+    const int share = max(2, (int)sqrtf((float)most * add));
+    const int G = (int)min((long long)n_workers, max(1ll, codes::divide(U, share)));
     bool idle = worker >= G || U == 0;
     long long u0 = idle ? 0 : codes::divide(U * worker, G), u1 = idle ? 0 : codes::divide(U * (worker + 1), G);
     // Few items: one for a CTA, if the longest is done before an even split and its merge.
@@ -304,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 base += all;
             }
         }
-        if (threadIdx.x == 0) s_units[0] = U, s_units[1] = u0;
+        if (threadIdx.x == 0) s_units[0] = U, s_units[1] = u0, s_shares = G;
     }
     __syncthreads();
     if (whole_items) u0 = 0, u1 = idle ? 0 : s_units[1];
@@ -811,7 +821,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
             // adds the others' results, which they leave in slots, to its own.
             auto ctas_of = [&](const Piece& p, int& n) {
                 const long long all = s_units[0], u = s_units[1] + p.item0 + kItem;
-                const int ctas = (int)min((long long)n_workers, max(1ll, all / 2));
+                const int ctas = s_shares;
                 auto cta_of = [&](long long v) { return (int)codes::divide((v + 1) * ctas - 1, all); };
                 const int first = cta_of(u);
                 n = cta_of(u + (long long)(p.steps - 1) * p.tiles) - first + 1;
