@@ -319,6 +319,32 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
     __syncthreads();
     if (whole_items) u0 = 0, u1 = idle ? 0 : s_units[1];
 
+    // ---- blocks that see no token: their rows are empty, or the base's. By the whole CTA where
+    // its share is short, else by a warp beside it (41 x 2 x 12840 rows of 64 over 12 tokens 186 us
+    // so, 197 first; 4 x 12 x 736 over 411 tokens 24 first, 53 so).
+    auto empties = [&](int at, int threads) {
+        for (long long x = blockIdx.x; x < items; x += gridDim.x) {
+            const int b = (int)(x % shape.blocks), hk = (int)(x / shape.blocks % c.Hk), i = (int)(x / shape.blocks / c.Hk);
+            if (shape.steps(shape.length(i), b) > 0) continue;
+            if (at == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
+            const int n = shape.block_rows(b);
+            for (int y = at; y < n * (D / 8); y += threads) {
+                const int r = b * shape.kRows + y / (D / 8), d = y % (D / 8) * 8;
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
+                    w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
+                *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
+            }
+            if (a.lse && a.lse != a.base_lse)
+                for (int y = at; y < n; y += threads) {
+                    const long long to = lse_place(i, hk, b * shape.kRows + y);
+                    a.lse[to] = a.base_lse ? a.base_lse[to] : -INFINITY;
+                }
+        }
+    };
+    const bool first = u1 - u0 < 64;
+    if (none && first) empties(threadIdx.x, kThreads);
+
     bool ok = true;
     // The readers' side of the ring: the n-th piece, and that a warp is done with it.
     auto piece = [&](int n, Piece& p) {
@@ -378,26 +404,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                     if (!some) break;
                 }
             }
-        } else if (warp == 1 && none) {
-            // ====== blocks that see no token: their rows are empty, or the base's ======
-            for (long long x = blockIdx.x; x < (long long)a.n * c.Hk * shape.blocks; x += gridDim.x) {
-                const int b = (int)(x % shape.blocks), hk = (int)(x / shape.blocks % c.Hk), i = (int)(x / shape.blocks / c.Hk);
-                if (shape.steps(shape.length(i), b) > 0) continue;
-                if (lane == 0 && a.seqs && (unsigned)a.seqs[i] >= (unsigned)c.S) atomicOr(c.head + kCacheStatus, kDevIndex);
-                const int n = shape.block_rows(b);
-                for (int y = lane; y < n * (D / 8); y += 32) {
-                    const int r = b * shape.kRows + y / (D / 8), d = y % (D / 8) * 8;
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (a.base_out && a.base_lse[lse_place(i, hk, r)] != -INFINITY)
-                        w = *reinterpret_cast<const uint4*>(a.base_out + place(a.o_st, i, hk, r) + d);
-                    *reinterpret_cast<uint4*>(a.out + place(a.o_st, i, hk, r) + d) = w;
-                }
-                if (a.lse && a.lse != a.base_lse)
-                    for (int y = lane; y < n; y += 32) {
-                        const long long at = lse_place(i, hk, b * shape.kRows + y);
-                        a.lse[at] = a.base_lse ? a.base_lse[at] : -INFINITY;
-                    }
-            }
+        } else if (warp == 1) {
+            if (none && !first) empties(lane, 32);
         } else if (warp == 3) {
             // ============================== codes ==============================
             int half = 0, pieces = 0;
