@@ -481,18 +481,23 @@ def msf_cache_grow(cache: int, seqs, counts, tokens: int, n: int, stream=None) -
 
 
 def _row_call(fn, where, cache, layer, k, v, seqs, at, stream, heads=None):
-    bf16 = (_torch or _get_torch()).bfloat16
-    shape = k.shape
+    torch = _torch or _get_torch()
+    bf16, shape, strides = torch.bfloat16, k.shape, k.stride()
     if len(shape) != 4:
         raise ValueError(f"{where}: k and v are [rows, tokens, kv_heads, head_dim]")
     n, tokens, kv_heads, dim = shape
     if heads is not None and heads != (kv_heads, dim):
         raise ValueError(f"rows of {(kv_heads, dim)} heads, where the cache holds {heads}")
-    strides = _rows(k, bf16, "k")
-    if not _alike(_rows(v, bf16, "v", shape), strides, shape):
-        raise ValueError(f"{where}: k and v have the same strides")
+    sequence, token, head, last = strides
+    # what nearly every call has is checked here; what is left is looked at one by one
+    if (last != 1 or (sequence | token | head) & 7 or v.stride() != strides or v.shape != shape or k.dtype != bf16
+            or v.dtype != bf16 or not k.is_cuda or not v.is_cuda):
+        strides = _rows(k, bf16, "k")
+        if not _alike(_rows(v, bf16, "v", shape), strides, shape):
+            raise ValueError(f"{where}: k and v have the same strides")
+        sequence, token, head = strides
     status = fn(cache, layer, None if seqs is None else _list(seqs, n)[0], None if at is None else _list(at, n)[0], n,
-                tokens, k.data_ptr(), v.data_ptr(), _STRIDES.pack(*strides), _stream(stream))
+                tokens, k.data_ptr(), v.data_ptr(), _STRIDES.pack(sequence, token, head), _stream(stream))
     if status:
         raise MsfError(status, where)
 
