@@ -2,7 +2,8 @@
 
 Each translation unit is compiled by nvcc in parallel into ``_build/`` at the
 repository root, then linked into ``paper_2607_20940_gb300/libmsf.so``.
-Objects are rebuilt only when a source or header is newer than them.
+Objects are rebuilt only when a source or header is newer than them. Where Python's
+headers are there, the binding's C module is compiled beside it.
 """
 from __future__ import annotations
 
@@ -11,12 +12,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmsf.so")
+CALLS = os.path.join(PKG, "_cache_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include")]
 
@@ -49,9 +52,25 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _build_calls() -> None:
+    src, include = os.path.join(CSRC, "cache_calls.c"), sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        return
+    newest = max(os.path.getmtime(p) for p in [src] + glob.glob(os.path.join(ROOT, "include", "*.h")))
+    if os.path.exists(CALLS) and os.path.getmtime(CALLS) >= newest:
+        return
+    tmp = CALLS + ".tmp"
+    r = subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-fPIC", "-shared", "-I", include, src, "-o", tmp], capture_output=True,
+                       text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compiling {src} failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cpp")))
+    _build_calls()
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
     newest = max(os.path.getmtime(o) for o in objs)

@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const CacheView
                 }
         }
     };
-    const bool first = u1 - u0 < 64;
+    const bool first = u1 - u0 < 24;
     if (none && first) empties(threadIdx.x, kThreads);
 
     bool ok = true;

@@ -403,12 +403,23 @@ def msf_kernel_launches() -> int:
 
 _torch = None
 
+# The calls of single tokens read their tensors in C where that was built (Python's
+# headers were there): 3 us a call of argument checks become 1.
+try:
+    from . import _cache_calls as _calls
+except ImportError:
+    _calls = None
+_WRITE, _READ, _ATTEND, _ATTEND_SIMT = (ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
+    "msf_cache_write", "msf_cache_read", "msf_cache_attend", "msf_cache_attend_simt"))
+
 
 def _get_torch():
     global _torch
     if _torch is None:
         import torch
         _torch = torch
+        if _calls is not None:
+            _calls.types(torch.bfloat16, torch.float32, torch.int32)
     return _torch
 
 
@@ -722,10 +733,22 @@ class Cache:
 
     def write(self, layer, k, v, seqs=None, counts=None, stream=None):
         """Quantise the newest tokens: k, v bf16 [rows, tokens, kv_heads, head_dim]."""
+        if _calls is not None:
+            status = _calls.rows(_WRITE, self.handle, layer, k, v, seqs, counts, self.kv_heads, self.head_dim, _stream(stream))
+            if status == MSF_OK:
+                return
+            if status is not None:
+                raise MsfError(status, "msf_cache_write")
         _row_call(_lib.msf_cache_write, "msf_cache_write", self.handle, layer, k, v, seqs, counts, stream, self.heads)
 
     def read(self, layer, k, v, seqs=None, begins=None, stream=None):
         """Read tokens from begins[i] on (0) back into bf16 k, v."""
+        if _calls is not None:
+            status = _calls.rows(_READ, self.handle, layer, k, v, seqs, begins, self.kv_heads, self.head_dim, _stream(stream))
+            if status == MSF_OK:
+                return
+            if status is not None:
+                raise MsfError(status, "msf_cache_read")
         _row_call(_lib.msf_cache_read, "msf_cache_read", self.handle, layer, k, v, seqs, begins, stream, self.heads)
 
     def fork(self, src, dst, lengths=None, copy=False, stream=None):
@@ -746,6 +769,13 @@ class Cache:
         """Attention of q [rows, queries, heads, head_dim] over the listed sequences, joined with
         (base_out, base_lse) where given; lse [rows, heads, queries]. skip: newest tokens that are not
         seen. simt: on fp32 CUDA cores."""
+        if _calls is not None:
+            status = _calls.attend(_ATTEND_SIMT if simt else _ATTEND, self.handle, layer, q, out, lse, base_out, base_lse,
+                                   seqs, causal, softmax_scale, skip, self.head_dim, _stream(stream))
+            if status == MSF_OK:
+                return
+            if status is not None:
+                raise MsfError(status, "msf_cache_attend_simt" if simt else "msf_cache_attend")
         torch = _torch or _get_torch()
         shape = q.shape
         if len(shape) != 4 or shape[3] != self.head_dim:

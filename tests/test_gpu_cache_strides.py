@@ -55,3 +55,36 @@ def test_refusals():
     with pytest.raises(ValueError, match="entries"):
         c.write(0, k, v, ints([0, 1]))
     ok(c)
+
+
+def test_either_binding(monkeypatch):
+    """The calls whose tensors are read in C and those that Python reads do the same and refuse the same."""
+    assert msf._calls is not None, "built where Python's headers are"
+    k, v, q = rows((3, 20, 2, 64), 1), rows((3, 20, 2, 64), 2), rows((3, 4, 6, 64), 3)
+    base, base_lse = rows(q.shape, 4), torch.randn(3, 6, 4, device="cuda")
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(msf, "_calls", None)
+        c = make(kv_heads=2, head_dim=64, sequences=3)
+        c.grow(None, ints([20, 3, 7]))
+        c.write(0, k, v, ints([0, 1, 2]), ints([20, 3, 7]))
+        k0, v0 = torch.empty_like(k), torch.empty_like(v)
+        c.read(0, k0, v0, ints([2, 0, 1]), ints([1, 0, 2]))
+        out, lse, joined, inside = torch.empty_like(q), torch.empty_like(base_lse), base.clone(), base_lse.clone()
+        c.attend(0, q, out, lse, seqs=ints([2, 2, 0]), causal=True, softmax_scale=0.3, skip=1)
+        c.attend(0, q, joined, inside, joined, inside, causal=False)
+        other = torch.empty_like(q)
+        c.attend(0, q, other, None, base, base_lse, simt=True)
+        ok(c)
+        got.append((k0, v0, out, lse, joined, inside, other))
+        for refused in (lambda: c.write(1, k, v), lambda: c.write(0, k, v, None, None, stream=0) or c.read(-1, k0, v0),
+                        lambda: c.attend(0, q, out, lse, skip=-1), lambda: c.attend(0, q, out, lse, base)):
+            with pytest.raises(msf.MsfError):
+                refused()
+        for refused in (lambda: c.attend(0, q[0], out, lse), lambda: c.attend(0, q, out[:, :3], lse),
+                        lambda: c.attend(0, q, out, lse.half()), lambda: c.attend(0, q, out, lse, base[:2], base_lse),
+                        lambda: c.attend(0, q, out, lse, seqs=ints([0])), lambda: c.read(0, k0[..., :32], v0[..., :32])):
+            with pytest.raises(ValueError):
+                refused()
+    assert all(torch.equal(x, y) for x, y in zip(*got))
