@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 
 #include "cache.h"
+#include "cache_codes.cuh"
 #include "internal.h"
 #include "kernels.h"
 #include "ptx.cuh"
@@ -73,16 +74,20 @@ __device__ __forceinline__ unsigned page_bits(const CacheView& c, int w) {
 // The lowest `want` free pages into c.free_list. False if there are fewer. One
 // block; the list is in place when it returns.
 __device__ bool find_free(const CacheView& c, int want, int* sh) {
-    const int words = (c.pages + 31) / 32;
+    __shared__ int first_of[kThreads];
+    __shared__ unsigned free_of[kThreads];
+    const int words = (c.pages + 31) / 32, lane = threadIdx.x % 32;
     int found = 0;
     for (int w0 = 0; w0 < words && found < want; w0 += kThreads) {
         const int w = w0 + (int)threadIdx.x;
-        unsigned f = w < words ? ~__ldcg(c.used + w) & page_bits(c, w) : 0u;
+        const unsigned f = w < words ? ~__ldcg(c.used + w) & page_bits(c, w) : 0u;
         int total;
-        int at = found + block_scan(__popc(f), sh, total);
-        while (f && at < want) {
-            c.free_list[at++] = 32 * w + __ffs(f) - 1;
-            f &= f - 1;
+        first_of[threadIdx.x] = found + block_scan(__popc(f), sh, total);
+        free_of[threadIdx.x] = f;
+        __syncthreads();
+        for (int i = threadIdx.x / 32; i < kThreads && first_of[i] < want; i += kThreads / 32) {  // a warp a word
+            const int at = first_of[i] + __popc(free_of[i] & ((1u << lane) - 1u));
+            if ((free_of[i] >> lane & 1u) && at < want) c.free_list[at] = 32 * (w0 + i) + lane;
         }
         found += total;
     }
@@ -249,11 +254,13 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     // The new rows, before any table changes. A warp takes 32 columns of a row at a time.
     const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
     for (long long x = warp; x < (long long)n * strips; x += warps) {
-        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
-        if (j >= min(cache_need(c, __ldcg(c.new_len + i)), c.W)) continue;
-        int page = __ldcg(c.table + (size_t)src[i] * c.W + j);
+        const int i = (int)codes::divide(x, strips), j = 32 * (int)(x - (long long)i * strips) + lane;
+        // (loads that do not wait for one another)
+        const int len = __ldcg(c.new_len + i), from = src[i], first = copy ? __ldcg(c.row + i) : 0;
+        int page = j < c.W ? __ldcg(c.table + (size_t)from * c.W + j) : -1;
+        if (j >= min(cache_need(c, len), c.W)) continue;
         if (copy) {
-            const int at = __ldcg(c.row + i) + j, own = __ldcg(c.free_list + at);
+            const int at = first + j, own = __ldcg(c.free_list + at);
             c.copies[at] = make_int2(page, own);
             take_page(c, own);
             page = own;
@@ -264,19 +271,19 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     }
     ptx::cluster_sync();
     for (long long x = warp; x < (long long)n * strips; x += warps) {
-        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
-        const int d = dst[i];
+        const int i = (int)codes::divide(x, strips), j = 32 * (int)(x - (long long)i * strips) + lane;
+        const int d = dst[i], len = __ldcg(c.new_len + i), k = min(cache_need(c, len), c.W);
         int* to = c.table + (size_t)d * c.W + j;
-        const int k = min(cache_need(c, __ldcg(c.new_len + i)), c.W);
         if (j < c.W) {
             const int old = __ldcg(to);  // -1 past the sequence's last page
-            if (old >= 0) drop_page(c, old);
+            const int page = __ldcg(c.stage + (size_t)i * c.W + j);  // (anything from k on)
             if (j < k)
-                *to = __ldcg(c.stage + (size_t)i * c.W + j);
+                *to = page;
             else if (old >= 0)
                 *to = -1;
+            if (old >= 0) drop_page(c, old);
         }
-        if (j == 0) c.lengths[d] = __ldcg(c.new_len + i);
+        if (j == 0) c.lengths[d] = len;
     }
 }
 
@@ -288,12 +295,13 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     ptx::cluster_sync();  // lengths change from here on
     const int warp = t / 32, lane = t % 32, warps = T / 32, strips = (c.W + 31) / 32;
     for (long long x = warp; x < (long long)n * strips; x += warps) {
-        const int i = (int)(x / strips), j = 32 * (int)(x - (long long)i * strips) + lane;
+        const int i = (int)codes::divide(x, strips), j = 32 * (int)(x - (long long)i * strips) + lane;
         const int s = seq_of(seqs, i), len = __ldcg(c.new_len + i);
         int* entry = c.table + (size_t)s * c.W + j;
-        if (j < c.W && j >= cache_need(c, len) && *entry >= 0) {
-            drop_page(c, *entry);
+        const int old = j < c.W ? *entry : -1;
+        if (old >= 0 && j >= cache_need(c, len)) {
             *entry = -1;
+            drop_page(c, old);
         }
         if (j == 0) c.lengths[s] = len;
     }
