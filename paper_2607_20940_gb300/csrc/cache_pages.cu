@@ -71,24 +71,34 @@ __device__ __forceinline__ unsigned page_bits(const CacheView& c, int w) {
     return n >= 32 ? 0xffffffffu : (1u << n) - 1u;
 }
 
+// f(rank, thread, bit) for the set bits of every thread's word, `first` the rank of its
+// lowest, below `limit`: a warp a word (a thread a word takes up to 32 turns). Every thread calls.
+template <class F>
+__device__ __forceinline__ void each_bit(unsigned word, int first, int limit, F f) {
+    __shared__ int first_of[kThreads];
+    __shared__ unsigned word_of[kThreads];
+    const int lane = threadIdx.x % 32;
+    first_of[threadIdx.x] = first;
+    word_of[threadIdx.x] = word;
+    __syncthreads();
+    for (int i = threadIdx.x / 32; i < kThreads && first_of[i] < limit; i += kThreads / 32) {
+        const int rank = first_of[i] + __popc(word_of[i] & ((1u << lane) - 1u));
+        if ((word_of[i] >> lane & 1u) && rank < limit) f(rank, i, lane);
+    }
+    __syncthreads();
+}
+
 // The lowest `want` free pages into c.free_list. False if there are fewer. One
 // block; the list is in place when it returns.
 __device__ bool find_free(const CacheView& c, int want, int* sh) {
-    __shared__ int first_of[kThreads];
-    __shared__ unsigned free_of[kThreads];
-    const int words = (c.pages + 31) / 32, lane = threadIdx.x % 32;
+    const int words = (c.pages + 31) / 32;
     int found = 0;
     for (int w0 = 0; w0 < words && found < want; w0 += kThreads) {
         const int w = w0 + (int)threadIdx.x;
         const unsigned f = w < words ? ~__ldcg(c.used + w) & page_bits(c, w) : 0u;
         int total;
-        first_of[threadIdx.x] = found + block_scan(__popc(f), sh, total);
-        free_of[threadIdx.x] = f;
-        __syncthreads();
-        for (int i = threadIdx.x / 32; i < kThreads && first_of[i] < want; i += kThreads / 32) {  // a warp a word
-            const int at = first_of[i] + __popc(free_of[i] & ((1u << lane) - 1u));
-            if ((free_of[i] >> lane & 1u) && at < want) c.free_list[at] = 32 * (w0 + i) + lane;
-        }
+        const int at = found + block_scan(__popc(f), sh, total);
+        each_bit(f, at, want, [&](int rank, int i, int bit) { c.free_list[rank] = 32 * (w0 + i) + bit; });
         found += total;
     }
     __syncthreads();
@@ -331,14 +341,14 @@ __global__ void __launch_bounds__(kThreads) cache_compact_kernel(const CacheView
         const unsigned u = w < words ? c.used[w] & page_bits(c, w) : 0u;
         const int below = min(32, max(0, live - 32 * w));  // bits that stand for pages below u
         const unsigned low = w < words ? (below == 32 ? 0xffffffffu : (1u << below) - 1u) : 0u;
-        unsigned f = ~u & low, m = u & ~low;
+        const unsigned f = ~u & low, m = u & ~low;
         int total;
         int at = holes + block_scan(__popc(f), sh, total);
         holes += total;
-        for (; f; f &= f - 1) c.copies[at++].y = 32 * w + __ffs(f) - 1;
+        if (total > 0) each_bit(f, at, holes, [&](int rank, int i, int bit) { c.copies[rank].y = 32 * (w0 + i) + bit; });
         at = high + block_scan(__popc(m), sh, total);
         high += total;
-        for (; m; m &= m - 1) c.copies[at++].x = 32 * w + __ffs(m) - 1;
+        if (total > 0) each_bit(m, at, high, [&](int rank, int i, int bit) { c.copies[rank].x = 32 * (w0 + i) + bit; });
     }
     __syncthreads();
     // holes == high: as many pages are missing below u as there are above it
