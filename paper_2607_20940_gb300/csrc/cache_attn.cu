@@ -157,11 +157,11 @@ __global__ void __launch_bounds__(128) cache_attend_kernel(const CacheView c, co
 // adds theirs in order (the same bits whichever is last).
 //
 // Measured, 128 dims: 64 sequences of up to 8191 tokens, 8 key heads, 4 queries each:
-// 284 MB in 62.9 us (4.5 TB/s, 0.66 of a copy's rate); one of 131071 tokens: 151 MB in
-// 37.2 us. An SM's four schedulers issue in 57% of the cycles; the conversions (2.8
+// 284 MB in 63.0 us (4.5 TB/s, 0.66 of a copy's rate); one of 131071 tokens: 151 MB in
+// 36.9 us. An SM's four schedulers issue in 57% of the cycles; the conversions (2.8
 // cycles a warp) and the f16 products that share a pipe with the scaling hold them up
-// more than HBM does, and a launch's ends (shares, joins) take 5 to 7 us: a list of two
-// short sequences 5.5 us.
+// more than HBM does, and a launch's ends (shares, joins) take 4 to 6 us: a list of two
+// short sequences 4.8 us.
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kItem = 1, kSplit = 4;
@@ -231,11 +231,11 @@ __device__ __forceinline__ void operand(uint32_t (&a)[4], uint32_t w0, uint32_t 
     a[3] = codes::mul_f16x2(codes::e2m1_f16x2<J>(w3), s3);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool kLong>
 struct FewCfg {
     static constexpr int kRows = 8 * NT;
-    // by the registers: 128, 168 or 255 a thread (64 dims, 20 rows: 16 warps spill)
-    static constexpr int kWarps = NT == 1 || D * NT < 192 ? 16 : D * NT <= 256 ? 12 : 8;
+    // Long calls: by the registers, 128, 168 or 255 a thread (64 dims, 20 rows: 16 warps spill).
+    static constexpr int kWarps = !kLong || D * NT > 256 ? 8 : NT == 1 || D * NT < 192 ? 16 : 12;
     static constexpr int kStages = 2;  // pairs of records in flight
     static constexpr int kPitch = D + 4;                        // floats of a row of outputs in shared memory
     static constexpr int kPart = kRows * (kPitch + 2) * 4;      // a piece's output, maxima and sums
@@ -244,14 +244,14 @@ struct FewCfg {
     static constexpr int kSmem = kWarps * (kOwn + kPart) + 128;
     static constexpr int kSlot = kRows * (D + 2);               // floats of a CTA's partial result
 };
-static_assert(FewCfg<128, 1>::kSmem <= 224 * 1024 && FewCfg<128, 2>::kSmem <= 224 * 1024 && FewCfg<128, 3>::kSmem <= 224 * 1024 &&
-                  FewCfg<64, 3>::kSmem <= 224 * 1024,
+static_assert(FewCfg<128, 1, true>::kSmem <= 224 * 1024 && FewCfg<128, 2, true>::kSmem <= 224 * 1024 &&
+                  FewCfg<128, 3, true>::kSmem <= 224 * 1024 && FewCfg<64, 3, true>::kSmem <= 224 * 1024,
               "shared memory of the launch");
 
-template <int D, int NT>
-__global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
+template <int D, int NT, bool kLong>
+__global__ void __launch_bounds__(32 * FewCfg<D, NT, kLong>::kWarps, 1)
     cache_few_kernel(const CacheView c, const CacheAttnArgs a) {
-    using C = FewCfg<D, NT>;
+    using C = FewCfg<D, NT, kLong>;
     constexpr int kW = C::kWarps, kT = 32 * kW, kS = C::kStages, kRec = cache_record_bytes(D);
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float s_w[2][kW][C::kRows];                 // weights of the warps' first and last pieces
@@ -855,31 +855,66 @@ __global__ void __launch_bounds__(32 * FewCfg<D, NT>::kWarps, 1)
             }
         }
         __syncthreads();
-        for (int y = threadIdx.x; y < rows * (D / 4); y += kT) {
-            const int r = y / (D / 4), d = y % (D / 4) * 4;
-            const float M = s_M[r];
+        // four dims of a row by as many lanes as there are, each every lanes-th piece
+        const int all = rows * (D / 4);
+        int lanes = 1;
+        while (lanes < 8 && 2 * lanes * all <= kT) lanes *= 2;
+        for (int y = threadIdx.x; (y & ~31) < all * lanes; y += kT) {
+            const int z0 = y / lanes, r = z0 / (D / 4), d = z0 % (D / 4) * 4;
+            const bool some = z0 < all;
+            const float M = some ? s_M[r] : 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-            for (int x = 0; x < n; ++x) {
-                const float w = codes::ex2(__ldcg(slot_of(x) + C::kRows * D + 2 * r) - M);
-                const float4 z = __ldcg(reinterpret_cast<const float4*>(slot_of(x) + r * D + d));
-                acc.x = fmaf(w, z.x, acc.x), acc.y = fmaf(w, z.y, acc.y), acc.z = fmaf(w, z.z, acc.z), acc.w = fmaf(w, z.w, acc.w);
+            constexpr int kAhead = 6;
+            for (int x0 = y % lanes; some && x0 < n; x0 += kAhead * lanes) {
+                float m4[kAhead];
+                float4 z[kAhead];
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (x0 + e * lanes < n) {
+                        m4[e] = __ldcg(slot_of(x0 + e * lanes) + C::kRows * D + 2 * r);
+                        z[e] = __ldcg(reinterpret_cast<const float4*>(slot_of(x0 + e * lanes) + r * D + d));
+                    }
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (x0 + e * lanes < n) {
+                        const float w = codes::ex2(m4[e] - M);
+                        acc.x = fmaf(w, z[e].x, acc.x), acc.y = fmaf(w, z[e].y, acc.y);
+                        acc.z = fmaf(w, z[e].z, acc.z), acc.w = fmaf(w, z[e].w, acc.w);
+                    }
             }
-            store(i, hb, r, d, acc, s_own[r % kW][r], s_other[r % kW][r]);
+            for (int e = 1; e < lanes; e *= 2) {
+                acc.x += __shfl_xor_sync(0xffffffffu, acc.x, e), acc.y += __shfl_xor_sync(0xffffffffu, acc.y, e);
+                acc.z += __shfl_xor_sync(0xffffffffu, acc.z, e), acc.w += __shfl_xor_sync(0xffffffffu, acc.w, e);
+            }
+            if (some && y % lanes == 0) store(i, hb, r, d, acc, s_own[r % kW][r], s_other[r % kW][r]);
         }
         __syncthreads();
     }
 }
 
+template <int D, int NT, bool kLong>
+cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, int sms, cudaStream_t st) {
+    using C = FewCfg<D, NT, kLong>;
+    const cudaError_t e = set_smem_attr((const void*)cache_few_kernel<D, NT, kLong>, C::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(cache_few_kernel<D, NT, kLong>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
+                      st, c, a);
+}
 template <int D, int NT>
 cudaError_t launch_few(const CacheView& c, const CacheAttnArgs& a, cudaStream_t st) {
-    using C = FewCfg<D, NT>;
     int sms;
-    cudaError_t e = device_sms(&sms);
-    if (e == cudaSuccess) e = set_smem_attr((const void*)cache_few_kernel<D, NT>, C::kSmem);
+    const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    return launch_pdl(cache_few_kernel<D, NT>, dim3(sms < kCacheMaxCtas ? sms : kCacheMaxCtas), dim3(32 * C::kWarps), C::kSmem,
-                      st, c, a);
+    // Eight warps where a CTA has few pairs, by what the sequences can hold: they start and
+    // join sooner (60 tokens 4.8 us, 5.5 with 16; 4 x 12 heads x 2500, 25 pairs a CTA, 10.5 and
+    // 13.2), but take codes apart slower (16 x 8 heads x 2000, 53 pairs, 14.9 and 13.1; 16 rows of 4 x
+    // 8 x 1000, 7 pairs, 11.3 and 13.0, 10 rows of 5 x 21461, 22 pairs, 32 and 18).
+    if constexpr (D * NT <= 256) {
+        const long long blocks = (a.group.d * a.queries + 8 * NT - 1) / (8 * NT);
+        const long long pairs = ((long long)c.W * c.P + 31) / 32 * blocks * a.n * c.Hk;
+        if (pairs > (NT == 1 ? 32ll : 12ll) * sms) return launch_few<D, NT, true>(c, a, sms, st);
+    }
+    return launch_few<D, NT, false>(c, a, sms, st);
 }
 
 }  // namespace
